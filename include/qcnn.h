@@ -77,7 +77,8 @@ typedef enum qcnn_status {
   QCNN_ERR_HIP = 5,         /* a HIP runtime call or kernel launch failed */
   QCNN_ERR_UNSUPPORTED = 6, /* C'_s > 16, codes not 4-byte aligned, grid or LDS limits */
   QCNN_ERR_ALIAS = 7,       /* an output overlaps an input */
-  QCNN_ERR_WORKSPACE = 8    /* qcnn_conv_forward_noalloc: the layer needs more than its static scratch */
+  QCNN_ERR_WORKSPACE = 8    /* qcnn_conv_forward_noalloc: the layer needs more than its static scratch;
+                               dense layers: the caller's workspace is too small */
 } qcnn_status;
 
 /* Build the table of sub-codeword inner products (Sec. 3.1 test phase;
@@ -350,6 +351,97 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
                          const float* T, int C_t, int d_k, int stride, int pad,
                          float* codebooks, int M, int K, int Csp, uint8_t* codes,
                          int sweeps, int inner, double* objective, void* stream);
+
+/* ---- Dense fully-connected layers: the layers that the quantized ones stand
+ * for, in the forms that language models use them in, forward and backward.
+ * A quantizer's user needs them beside the quantized forward: for the
+ * original layer's responses (the T of qcnn_ec_fc), to train the weights that
+ * are quantized later, and for the loss that quantization costs.
+ *
+ * Types: `dtype` is the type T of every array declared void* (fp32, bf16 or
+ * fp16); sums, softmax statistics, loss and lse are fp32; a result is rounded
+ * to T once.  The backward calls round one intermediate to T as well, the
+ * operand of the matrix products (dz; the logits' gradient).
+ * Layouts: x [N][C_s], w [C_t][C_s], y, dy, residual [N][C_t].  x, y, dy and
+ * residual have row strides ldx, ldy, lddy, ldr in elements (at least their
+ * columns); everything else is contiguous.  Pointers are aligned to their
+ * element.  Rows of whole 16 bytes at 16-byte aligned addresses are read in
+ * place; otherwise x and w are first copied into the workspace.
+ * Limits: N <= 2^21; C_s, C_t (2 C_t of the gated layer) and strides <= 2^20;
+ * no more than 2^23 tiles of 128 x 128 in any of the products
+ * (QCNN_ERR_UNSUPPORTED past them).  Sizes are at least 1.
+ * Workspace: with workspace_bytes NULL the library's per-stream workspace is
+ * used.  With workspace NULL and workspace_bytes not NULL the call only
+ * writes the size that it needs there (0: none) and launches nothing.  With
+ * both, temporaries live in the caller's buffer of *workspace_bytes bytes
+ * (256-byte aligned; QCNN_ERR_WORKSPACE if too small): for calls captured
+ * into graphs that may run at the same time, each of which needs its own.
+ * Results do not depend on the choice, and are the same in every run. */
+typedef enum qcnn_dtype { QCNN_F32 = 0, QCNN_BF16 = 1, QCNN_F16 = 2 } qcnn_dtype;
+
+/* act(z): z; max(z, 0); z Phi(z) with the normal distribution function Phi;
+ * the same with (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 for Phi;
+ * z / (1 + exp(-z)).  relu's slope at 0 is 0. */
+typedef enum qcnn_act {
+  QCNN_ACT_NONE = 0,
+  QCNN_ACT_RELU = 1,
+  QCNN_ACT_GELU = 2,
+  QCNN_ACT_GELU_TANH = 3,
+  QCNN_ACT_SILU = 4
+} qcnn_act;
+
+/* z = x w^T + bias, y = act(z) + residual.  bias [C_t], residual, and pre
+ * (output: z, [N][C_t], which the backward call needs unless act is none) may
+ * be NULL. */
+qcnn_status qcnn_linear_forward(int dtype, const void* x, long long ldx, int N, int C_s, const void* w, int C_t,
+                                const void* bias, int act, const void* residual, long long ldr, void* pre, void* y,
+                                long long ldy, void* workspace, size_t* workspace_bytes, void* stream);
+
+/* Gradients of qcnn_linear_forward: dz = dy act'(pre), dx = dz w [N][C_s],
+ * dw = dz^T x [C_t][C_s], dbias = sum over rows of dz [C_t]; the residual's
+ * gradient is dy itself.  Each of dx, dw, dbias may be NULL, not all three;
+ * w is only needed for dx, x for dw, pre unless act is none. */
+qcnn_status qcnn_linear_backward(int dtype, const void* dy, long long lddy, const void* x, long long ldx, int N,
+                                 int C_s, const void* w, int C_t, const void* pre, int act, void* dx, void* dw,
+                                 void* dbias, void* workspace, size_t* workspace_bytes, void* stream);
+
+/* The gated feed-forward layer: with w [2 C_t][C_s], rows 0 .. C_t - 1 the
+ * gate's and the rest the up projection's, and bias [2 C_t] or NULL,
+ *   [g u] = x w^T + bias,   y = act(g) u   [N][C_t].
+ * pre (output, may be NULL): [g u], [N][2 C_t].  The block's last projection,
+ * with the residual, is qcnn_linear_forward. */
+qcnn_status qcnn_gated_forward(int dtype, const void* x, long long ldx, int N, int C_s, const void* w, int C_t,
+                               const void* bias, int act, void* pre, void* y, long long ldy, void* workspace,
+                               size_t* workspace_bytes, void* stream);
+
+/* Gradients of qcnn_gated_forward: dg = dy u act'(g), du = dy act(g),
+ * dx = [dg du] w, dw = [dg du]^T x [2 C_t][C_s], dbias [2 C_t].  NULLs as in
+ * qcnn_linear_backward, but pre is always needed. */
+qcnn_status qcnn_gated_backward(int dtype, const void* dy, long long lddy, const void* x, long long ldx, int N,
+                                int C_s, const void* w, int C_t, const void* pre, int act, void* dx, void* dw,
+                                void* dbias, void* workspace, size_t* workspace_bytes, void* stream);
+
+/* A classifying layer with its softmax cross entropy, over C_t classes (a
+ * vocabulary): z = x w^T + bias,
+ *   lse[n] = log sum_c exp z[n][c],   loss[n] = lse[n] - z[n][labels[n]].
+ * The logits are never stored: each tile of classes leaves its maximum and
+ * sum per row.  labels [N] int64; a negative label leaves its row out (loss
+ * and gradients 0, lse as usual); one >= C_t makes the row's loss and every
+ * gradient that it enters NaN.  A bias of -infinity takes its class out. */
+qcnn_status qcnn_linear_xent_forward(int dtype, const void* x, long long ldx, int N, int C_s, const void* w, int C_t,
+                                     const void* bias, const int64_t* labels, float* loss, float* lse,
+                                     void* workspace, size_t* workspace_bytes, void* stream);
+
+/* Gradients of sum_n dloss[n] loss[n] (dloss [N] fp32; 1 / count for a mean):
+ * d[n][c] = dloss[n] (exp(z[n][c] - lse[n]) - [c = labels[n]]),
+ * dx = d w, dw = d^T x, dbias = sum over rows of d, from the forward call's
+ * lse.  The logits are computed again, for as many classes at a time as fit
+ * 256 MiB (256 classes at least).  NULLs as in qcnn_linear_backward; x and w
+ * are always needed. */
+qcnn_status qcnn_linear_xent_backward(int dtype, const float* dloss, const float* lse, const void* x, long long ldx,
+                                      int N, int C_s, const void* w, int C_t, const void* bias,
+                                      const int64_t* labels, void* dx, void* dw, void* dbias, void* workspace,
+                                      size_t* workspace_bytes, void* stream);
 
 /* Network glue between PQ layers (not part of the paper's method): max
  * pooling over k x k windows with stride s and no padding,

@@ -11,7 +11,8 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqcnn.so")
 
-P, I = ctypes.c_void_p, ctypes.c_int
+P, I, L = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong
+Z = ctypes.POINTER(ctypes.c_size_t)
 
 # Entry points declared in include/qcnn.h, with their argument types.
 SIGNATURES = {
@@ -45,6 +46,12 @@ SIGNATURES = {
     "qcnn_probe_valu": ([ctypes.POINTER(ctypes.c_double)] * 3 + [P], I),
     "qcnn_probe_lds": ([ctypes.POINTER(ctypes.c_double)] * 3 + [P], I),
     "qcnn_probe_hbm": ([P, P, ctypes.c_size_t] + [ctypes.POINTER(ctypes.c_double)] * 3 + [P], I),
+    "qcnn_linear_forward": ([I, P, L, I, I, P, I, P, I, P, L, P, P, L, P, Z, P], I),
+    "qcnn_linear_backward": ([I, P, L, P, L, I, I, P, I, P, I, P, P, P, P, Z, P], I),
+    "qcnn_gated_forward": ([I, P, L, I, I, P, I, P, I, P, P, L, P, Z, P], I),
+    "qcnn_gated_backward": ([I, P, L, P, L, I, I, P, I, P, I, P, P, P, P, Z, P], I),
+    "qcnn_linear_xent_forward": ([I, P, L, I, I, P, I, P, P, P, P, P, Z, P], I),
+    "qcnn_linear_xent_backward": ([I, P, P, P, L, I, I, P, I, P, P, P, P, P, P, Z, P], I),
     "qcnn_timing_read": ([ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_longlong)], I),
 }
 

@@ -597,3 +597,220 @@ def pq_kmeans(W: torch.Tensor, init_codebooks: torch.Tensor, iters: int):
     check(lib().qcnn_pq_kmeans(W.data_ptr(), Ct, Cs, dk, M, K, Csp, int(iters), D.data_ptr(), codes.data_ptr(),
                                objective.data_ptr(), _stream(W)), "qcnn_pq_kmeans")
     return D, codes, objective
+
+
+# ------------------------------------------------ dense fully-connected layers
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _dtype(x: torch.Tensor, name: str) -> int:
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, x.dtype))
+    return code
+
+
+def _act(act: str) -> int:
+    code = _ACTS.get(act)
+    if code is None:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(_ACTS), act))
+    return code
+
+
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, shape, device=None) -> int:
+    """A matrix whose rows are contiguous, at any distance: that distance."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, shape or "[rows][columns]", tuple(t.shape)))
+    if not t.is_cuda:
+        raise ValueError("%s must be on a GPU device" % name)
+    if device is not None and t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    n, c = t.shape
+    s = t.stride()
+    if (c > 1 and s[1] != 1) or (n > 1 and s[0] < c):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return s[0] if n > 1 else c
+
+
+def _vector(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, device) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t, name, dtype, 1, device)
+    if t.shape[0] != n:
+        raise ValueError("%s must have %d entries, got %d" % (name, n, t.shape[0]))
+    return t.data_ptr()
+
+
+def _dense_call(entry: str, device, args) -> None:
+    """One call on the device's current stream.  A call that is being captured
+    into a graph gets a workspace of its own from torch, which the graph's
+    memory pool keeps: graphs captured on one stream may then be replayed at
+    the same time.  Any other call uses the library's workspace of its stream."""
+    f = getattr(lib(), entry)
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _dense_call(entry, device, args)
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if not torch.cuda.is_current_stream_capturing():
+        return check(f(*args, None, None, stream), entry)
+    size = ctypes.c_size_t(0)
+    check(f(*args, None, ctypes.byref(size), stream), entry)
+    room = torch.empty(max(1, size.value), dtype=torch.uint8, device=device)
+    check(f(*args, room.data_ptr(), ctypes.byref(size), stream), entry)
+
+
+def _dense_wx(x: torch.Tensor, w: torch.Tensor, halves: int = 1):
+    """(dtype code, row stride of x, N, C_s, C_t) of a layer's input and weight."""
+    dt = _dtype(x, "x")
+    ldx = _rows(x, "x", x.dtype, None)
+    _need(w, "w", x.dtype, 2, x.device)
+    N, Cs = x.shape
+    if w.shape[1] != Cs or w.shape[0] % halves:
+        raise ValueError("w has shape %s, expected [%s][C_s=%d]" % (tuple(w.shape), "C_t" if halves == 1 else "2 C_t",
+                                                                     Cs))
+    return dt, ldx, N, Cs, w.shape[0] // halves
+
+
+def _output(out: Optional[torch.Tensor], name: str, like: torch.Tensor, shape) -> Tuple[torch.Tensor, int]:
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device), shape[1]
+    return out, _rows(out, name, like.dtype, shape, like.device)
+
+
+def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
+                   residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   pre: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Dense fully-connected layer, y = act(x w^T + bias) + residual
+    (qcnn_linear_forward).
+
+    x [N][C_s], w [C_t][C_s], bias [C_t] or None, residual [N][C_t] or None, all
+    of one type (float32, bfloat16 or float16); act "none", "relu", "gelu",
+    "gelu_tanh" or "silu".  x, residual and out may be rows of wider arrays.
+    pre [N][C_t], if given, receives x w^T + bias for linear_backward.
+    Returns y [N][C_t].
+    """
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w)
+    bp = _vector(bias, "bias", x.dtype, Ct, x.device)
+    ldr = 0 if residual is None else _rows(residual, "residual", x.dtype, (N, Ct), x.device)
+    if pre is not None:
+        _need_shaped(pre, "pre", x.dtype, (N, Ct), x.device)
+    out, ldy = _output(out, "out", x, (N, Ct))
+    _dense_call("qcnn_linear_forward", x.device,
+                (dt, x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, bp, _act(act),
+                 None if residual is None else residual.data_ptr(), ldr, None if pre is None else pre.data_ptr(),
+                 out.data_ptr(), ldy))
+    return out
+
+
+def _gradient_outputs(like, N, Cs, rows, need_dx, need_dw, need_dbias):
+    if not (need_dx or need_dw or need_dbias):
+        raise ValueError("at least one gradient must be asked for")
+    new = lambda *shape: torch.empty(shape, dtype=like.dtype, device=like.device)  # noqa: E731
+    return (new(N, Cs) if need_dx else None, new(rows, Cs) if need_dw else None, new(rows) if need_dbias else None)
+
+
+def _pointers(*tensors):
+    return [None if t is None else t.data_ptr() for t in tensors]
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, act: str = "none",
+                    pre: Optional[torch.Tensor] = None, need_dx: bool = True, need_dw: bool = True,
+                    need_dbias: bool = True):
+    """Gradients of linear_forward (qcnn_linear_backward): with dz = dy act'(pre),
+    (dx = dz w, dw = dz^T x, dbias = sum of dz over rows), None for what was
+    not asked for.  dy [N][C_t]; pre is what linear_forward wrote (not needed
+    with act "none").  The residual's gradient is dy."""
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w)
+    lddy = _rows(dy, "dy", x.dtype, (N, Ct), x.device)
+    code = _act(act)
+    if pre is not None:
+        _need_shaped(pre, "pre", x.dtype, (N, Ct), x.device)
+    grads = _gradient_outputs(x, N, Cs, Ct, need_dx, need_dw, need_dbias)
+    _dense_call("qcnn_linear_backward", x.device,
+                (dt, dy.data_ptr(), lddy, x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, *_pointers(pre), code,
+                 *_pointers(*grads)))
+    return grads
+
+
+def gated_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "silu",
+                  out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gated feed-forward layer, y = act(g) u with [g u] = x w^T + bias
+    (qcnn_gated_forward): both projections, the activation and the product in
+    one call.
+
+    x [N][C_s], w [2 C_t][C_s] (the gate's rows, then the up projection's), bias
+    [2 C_t] or None; types, act and strides as in linear_forward.  pre
+    [N][2 C_t], if given, receives [g u] for gated_backward.  Returns y
+    [N][C_t]; linear_forward is the block's last projection.
+    """
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w, 2)
+    bp = _vector(bias, "bias", x.dtype, 2 * Ct, x.device)
+    if pre is not None:
+        _need_shaped(pre, "pre", x.dtype, (N, 2 * Ct), x.device)
+    out, ldy = _output(out, "out", x, (N, Ct))
+    _dense_call("qcnn_gated_forward", x.device,
+                (dt, x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, bp, _act(act), None if pre is None else pre.data_ptr(),
+                 out.data_ptr(), ldy))
+    return out
+
+
+def gated_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: torch.Tensor, act: str = "silu",
+                   need_dx: bool = True, need_dw: bool = True, need_dbias: bool = True):
+    """Gradients of gated_forward (qcnn_gated_backward): (dx [N][C_s], dw
+    [2 C_t][C_s], dbias [2 C_t]), None for what was not asked for.  dy [N][C_t];
+    pre is what gated_forward wrote."""
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w, 2)
+    lddy = _rows(dy, "dy", x.dtype, (N, Ct), x.device)
+    _need_shaped(pre, "pre", x.dtype, (N, 2 * Ct), x.device)
+    grads = _gradient_outputs(x, N, Cs, 2 * Ct, need_dx, need_dw, need_dbias)
+    _dense_call("qcnn_gated_backward", x.device,
+                (dt, dy.data_ptr(), lddy, x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, pre.data_ptr(), _act(act),
+                 *_pointers(*grads)))
+    return grads
+
+
+def linear_xent_forward(x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, bias: Optional[torch.Tensor] = None):
+    """Softmax cross entropy of a classifying layer's logits x w^T + bias
+    (qcnn_linear_xent_forward), without storing them.
+
+    x [N][C_s], w [C_t][C_s], bias [C_t] or None; labels int64 [N], a negative
+    one leaving its row out (loss 0).  Returns (loss, lse), float32 [N]: each
+    row's loss and log-sum-exp.
+    """
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w)
+    bp = _vector(bias, "bias", x.dtype, Ct, x.device)
+    lp = _vector(labels, "labels", torch.int64, N, x.device)
+    if lp is None:
+        raise TypeError("labels must be a torch.Tensor")
+    loss = torch.empty(N, dtype=torch.float32, device=x.device)
+    lse = torch.empty(N, dtype=torch.float32, device=x.device)
+    _dense_call("qcnn_linear_xent_forward", x.device,
+                (dt, x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, bp, lp, loss.data_ptr(), lse.data_ptr()))
+    return loss, lse
+
+
+def linear_xent_backward(dloss: torch.Tensor, lse: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
+                         labels: torch.Tensor, bias: Optional[torch.Tensor] = None, need_dx: bool = True,
+                         need_dw: bool = True, need_dbias: Optional[bool] = None):
+    """Gradients of sum_n dloss[n] loss[n] of linear_xent_forward
+    (qcnn_linear_xent_backward): (dx, dw, dbias), None for what was not asked
+    for (dbias by default only where there is a bias).  dloss float32 [N], 1 /
+    count for a mean; lse is the forward call's."""
+    dt, ldx, N, Cs, Ct = _dense_wx(x, w)
+    bp = _vector(bias, "bias", x.dtype, Ct, x.device)
+    _need_shaped(labels, "labels", torch.int64, (N,), x.device)
+    _need_shaped(dloss, "dloss", torch.float32, (N,), x.device)
+    _need_shaped(lse, "lse", torch.float32, (N,), x.device)
+    grads = _gradient_outputs(x, N, Cs, Ct, need_dx, need_dw, bias is not None if need_dbias is None else need_dbias)
+    _dense_call("qcnn_linear_xent_backward", x.device,
+                (dt, dloss.data_ptr(), lse.data_ptr(), x.data_ptr(), ldx, N, Cs, w.data_ptr(), Ct, bp,
+                 labels.data_ptr(), *_pointers(*grads)))
+    return grads

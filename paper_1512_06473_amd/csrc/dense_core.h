@@ -1,0 +1,533 @@
+// Dense products on the matrix cores with fused epilogues: the core shared by
+// the linear, gated and classifying layers (dense_kernels.h).
+//
+//   out[q][p] = sum_k P(p, k) Q(q, k),   p contiguous in memory
+//
+// Each operand is stored along k ([rows][k], "C") or across it ([k][rows],
+// "S"): a forward pass is C x C, an input gradient S x C, a weight gradient
+// S x S.  A workgroup computes BP x BQ outputs; k runs in steps of 128 bytes.
+// Both tiles of a step go from memory straight to LDS (16 bytes per lane),
+// double-buffered, one barrier per step.
+//
+// A fragment is 16 bytes per lane: lane (g = lane / 16, i = lane % 16) holds
+// row i and the k's 8 g .. 8 g + 7 of 32 (16-bit types, one MFMA 16x16x32) or
+// 4 g .. 4 g + 3 of 16 (fp32, four MFMA 16x16x4, the n-th taking element n of
+// every lane; both operands agree on the order of k, which is free).
+//   C: one 128-bit LDS read.  Rows are 128 bytes; chunk c (16 bytes) of row r
+//      lies at c ^ ((r >> 1) & 7), so that 16 rows' reads cover all banks.
+//   S: transposed LDS reads (16-bit) or one dword per k (fp32).  Row k's
+//      chunk c lies at c ^ swizzle(k), spreading the rows of one read.
+// MFMA's first operand is P: a lane ends up with 4 consecutive p of one q.
+//
+// Bounds: an operand is read through a buffer descriptor whose extent ends
+// with its last element, so rows past the end read as 0; the tail of k is
+// cut off lane by lane (C) or by the extent (S).  p and q past the end are
+// not stored.
+#pragma once
+
+#include "qcnn_internal.h"
+
+namespace qcnn {
+namespace dense {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Transposing LDS read: with 16 lanes' addresses on 4 rows of 16 elements (lane
+// i: row i / 4, elements 4 (i % 4) ..), lane i receives element i of each row.
+__device__ __forceinline__ s4 read_transposed(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p);
+}
+
+template <typename T>
+struct Num;
+
+template <>
+struct Num<float> {
+  typedef f4 Frag;
+  typedef f4 Quad;
+  static __device__ __forceinline__ f4 mma(Frag a, Frag b, f4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ float exp_(float x) { return expf(x); }
+  static __device__ __forceinline__ float div_(float a, float b) { return a / b; }
+};
+
+// 16-bit results carry 8 or 11 bits: the hardware's exponential and reciprocal
+// (about 2^-22) are far below their rounding.
+struct Num16 {
+  static __device__ __forceinline__ float exp_(float x) { return __expf(x); }
+  static __device__ __forceinline__ float div_(float a, float b) { return a * __builtin_amdgcn_rcpf(b); }
+};
+
+template <>
+struct Num<__bf16> : Num16 {
+  typedef b8 Frag;
+  typedef b4 Quad;
+  static __device__ __forceinline__ f4 mma(Frag a, Frag b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ b4 read_tr(const char* p) {
+    return __builtin_bit_cast(b4, read_transposed(p));
+  }
+};
+
+template <>
+struct Num<_Float16> : Num16 {
+  typedef h8 Frag;
+  typedef h4 Quad;
+  static __device__ __forceinline__ f4 mma(Frag a, Frag b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ h4 read_tr(const char* p) {
+    return __builtin_bit_cast(h4, read_transposed(p));
+  }
+};
+
+// ------------------------------------------------------------- activations
+
+template <typename T>
+__device__ __forceinline__ float act_value(int act, float z) {
+  switch (act) {
+    case QCNN_ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
+    case QCNN_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case QCNN_ACT_GELU_TANH: {  // 1 + tanh(u) = 2 / (1 + exp(-2 u))
+      const float u2 = 1.5957691216057308f * (z + 0.044715f * z * z * z);
+      return Num<T>::div_(z, 1.f + Num<T>::exp_(-u2));
+    }
+    case QCNN_ACT_SILU: return Num<T>::div_(z, 1.f + Num<T>::exp_(-z));
+    default: return z;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ float act_slope(int act, float z) {
+  switch (act) {
+    case QCNN_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+    case QCNN_ACT_GELU:
+      return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + 0.39894228040143268f * z * Num<T>::exp_(-0.5f * z * z);
+    case QCNN_ACT_GELU_TANH: {
+      const float s = Num<T>::div_(1.f, 1.f + Num<T>::exp_(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
+      return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);
+    }
+    case QCNN_ACT_SILU: {
+      const float s = Num<T>::div_(1.f, 1.f + Num<T>::exp_(-z));
+      return s * (1.f + z * (1.f - s));
+    }
+    default: return 1.f;
+  }
+}
+
+// --------------------------------------------------------------- epilogues
+
+enum EpiKind { kLinear = 0, kPartial = 1, kGated = 2, kStats = 3, kXgrad = 4 };
+
+// What becomes of a sum.  Quads are 4 consecutive p; with `vec` every array of
+// T here may be read and written 4 at a time where 4 are left.
+struct Epi {
+  void* y;          // T [nq][ldy]: the result (kXgrad: the logits' gradient)
+  void* pre;        // T [nq][ldpre] or null: the sum with its bias
+  const void* bias; // T [np] (kGated: [2 np]) or null
+  const void* res;  // T [nq][ldr] or null: added last
+  float* acc;       // fp32 [nq][ldacc]: running sums over pieces of k, or null
+  const float* alpha;  // device scalar that the finished sum is multiplied by, or null
+  long long ldy, ldpre, ldr, ldacc;
+  int act;
+  int acc_in, acc_out;  // add what is in acc; leave the sum there (no y)
+  int vec;
+  // kStats, kXgrad: classes class0 .. class0 + np - 1 of `classes`
+  const long long* labels;
+  const float* lse;
+  const float* dloss;
+  const float* dmax;  // device scalar: the largest |dloss| (1 where that is 0)
+  float gain;
+  float2* stat;       // [slot][nq]: maximum and sum of exponentials of a slot's logits
+  float* zlabel;      // [nq]: the label's logit
+  int class0, classes;
+};
+
+template <typename T>
+__device__ __forceinline__ f4 load_quad(const T* p, bool full, int n) {
+  typedef typename Num<T>::Quad Quad;
+  f4 v = {0.f, 0.f, 0.f, 0.f};
+  if (full) {
+    const Quad t = *reinterpret_cast<const Quad*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) v[i] = (float)p[i];
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_quad(T* p, f4 v, bool full, int n) {
+  typedef typename Num<T>::Quad Quad;
+  if (full) {
+    Quad t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
+    *reinterpret_cast<Quad*>(p) = t;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void emit_linear(const Epi& e, int np, int q, int p, f4 v) {
+  const int n = np - p;
+  if (n <= 0) return;
+  const bool full = e.vec && n >= 4;
+  if (e.acc_in) v += *reinterpret_cast<const f4*>(e.acc + q * e.ldacc + p);
+  if (e.acc_out) {
+    *reinterpret_cast<f4*>(e.acc + q * e.ldacc + p) = v;
+    return;
+  }
+  if (e.alpha) v *= *e.alpha;
+  if (e.bias) v += load_quad(static_cast<const T*>(e.bias) + p, full, n);
+  if (e.pre) store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, v, full, n);
+  if (e.act != QCNN_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = act_value<T>(e.act, v[i]);
+  }
+  if (e.res) v += load_quad(static_cast<const T*>(e.res) + q * e.ldr + p, full, n);
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, v, full, n);
+}
+
+// np: columns of the result (half of the weight's rows).
+template <typename T>
+__device__ __forceinline__ void emit_gated(const Epi& e, int np, int q, int p, f4 g, f4 u) {
+  const int n = np - p;
+  if (n <= 0) return;
+  const bool full = e.vec && n >= 4;
+  if (e.bias) {
+    g += load_quad(static_cast<const T*>(e.bias) + p, full, n);
+    u += load_quad(static_cast<const T*>(e.bias) + np + p, full, n);
+  }
+  if (e.pre) {
+    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, g, full, n);
+    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + np + p, u, full, n);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) g[i] = act_value<T>(e.act, g[i]) * u[i];
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, g, full, n);
+}
+
+// Logits with their bias; classes past the end become -inf.
+template <typename T>
+__device__ __forceinline__ f4 class_logits(const Epi& e, int np, int p, f4 v) {
+  const int n = np - p;
+  if (e.bias && n > 0) v += load_quad(static_cast<const T*>(e.bias) + e.class0 + p, e.vec && n >= 4, n);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i >= n) v[i] = -INFINITY;
+  return v;
+}
+
+// d = dloss (softmax - onehot), divided by the largest |dloss| (the products
+// that read d multiply it back) so that a mean's 1 / N neither leaves a 16-bit
+// type's range nor rounds every label's entry the same way; times `gain`, a
+// power of two that keeps fp16's small probabilities off its subnormals.
+// y's rows are whole quads: what lies past np is written as 0.
+template <typename T>
+__device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int q, int p, f4 z) {
+  const long long label = e.labels[q];
+  z = class_logits<T>(e, np, p, z);
+  f4 d = {0.f, 0.f, 0.f, 0.f};
+  if (label >= 0) {
+    const float w = e.dloss[q] / *e.dmax * e.gain, lse = e.lse[q];
+    const long long at = label - e.class0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < np) d[i] = w * (Num<T>::exp_(z[i] - lse) - (at == p + i ? 1.f : 0.f));
+    if (label >= e.classes) d = f4{NAN, NAN, NAN, NAN};
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (p + i >= np) d[i] = 0.f;
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, d, true, 4);
+}
+
+// (max, sum of exp(. - max)) of two disjoint sets.
+__device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x);
+  if (m == -INFINITY) return make_float2(m, a.y + b.y);  // both empty (sums 0)
+  const float sa = a.x == -INFINITY ? 0.f : a.y * __expf(a.x - m);
+  const float sb = b.x == -INFINITY ? 0.f : b.y * __expf(b.x - m);
+  return make_float2(m, sa + sb);
+}
+
+// ------------------------------------------------------------- the product
+
+struct Prod {
+  const char* p;
+  const char* q;
+  long long ldp, ldq;   // bytes
+  int np, nq, nk;       // outputs and terms; nk of a C operand in whole 16 bytes
+  int kp, kq;           // rows that an S operand has (C: unused)
+  int colsp, colsq;     // columns that an S operand stores, whole 16 bytes
+  int p2;               // kGated: rows between a gate row and its up row
+  int splits, steps;    // parts of k; steps of 128 bytes in each
+  float* part;          // kPartial: fp32 [splits][nq][ldpart]
+  long long ldpart;     // kGated's sums: gate at p, up at ldpart / 2 + p
+};
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const char* base, long long bytes) {
+  const long long cap = 0x7fffffffLL;
+  const int num = (int)(bytes < 0 ? 0 : bytes > cap ? cap : bytes);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, num, 0x00020000);
+}
+
+// An operand's tile of ROWS rows: staging and fragments.
+template <typename T, bool S, int ROWS, int NW>
+struct Operand {
+  static constexpr int kS = sizeof(T);
+  static constexpr int kStep = 128 / kS;                   // k's of a step
+  static constexpr int kRowBytes = S ? ROWS * kS : 128;    // LDS row
+  static constexpr int kPerRow = kRowBytes / 16;           // chunks of an LDS row
+  static constexpr int kRowsPer = 64 / kPerRow;            // LDS rows of one wave's load
+  static constexpr int kLoads = ROWS * 128 / 1024 / NW;    // loads of one wave and step
+  static constexpr int kBytes = ROWS * 128;
+  static_assert(kLoads >= 1 && kLoads * NW * 1024 == ROWS * 128, "whole loads");
+  static_assert(!S || kRowBytes >= 256, "the swizzle of S tiles spans 256 bytes");
+  static_assert(kPerRow <= 64, "a row per load at least");
+
+  // XOR on the chunk index of LDS row r.
+  static __device__ __forceinline__ int swizzle(int r) {
+    if (!S) return (r >> 1) & 7;
+    if (kS == 2) return 2 * ((r & 3) | (((r >> 3) & 1) << 2));
+    return 4 * ((r >> 2) & 3);
+  }
+
+  // Offset of lane's 16 bytes of load j from the tile's first byte in memory.
+  // LDS row r is the operand's row r (gated: see row_of in the kernel).
+  static __device__ __forceinline__ int lds_row(int wave, int lane, int j) {
+    return (wave + j * NW) * kRowsPer + lane / kPerRow;
+  }
+  static __device__ __forceinline__ int chunk(int wave, int lane, int j) {
+    return (lane % kPerRow) ^ swizzle(lds_row(wave, lane, j));
+  }
+
+  // Fragment f (16 rows from row `at` + 16 f) of the kk-th part of a step.
+  static __device__ __forceinline__ typename Num<T>::Frag frag(const char* lds, int lane, int at, int f, int kk) {
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (!S) {
+      const int r = at + f * 16 + i;
+      return *reinterpret_cast<const typename Num<T>::Frag*>(lds + r * 128 + (((kk * 4 + g) ^ (i >> 1)) << 4));
+    } else if constexpr (kS == 2) {
+      const int k = kk * 32 + 8 * g + (i >> 2);
+      const int c = (((at + f * 16) >> 3) + ((i & 3) >> 1)) ^ (2 * ((i >> 2) | ((g & 1) << 2)));
+      const char* a = lds + k * kRowBytes + c * 16 + (i & 1) * 8;
+      const auto lo = Num<T>::read_tr(a), hi = Num<T>::read_tr(a + 4 * kRowBytes);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int k = kk * 16 + 4 * g;
+      const int col = at + f * 16 + i;
+      const char* a = lds + k * kRowBytes + ((col >> 2) ^ (4 * g)) * 16 + (col & 3) * 4;
+      f4 v;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] = *reinterpret_cast<const float*>(a + n * kRowBytes);
+      return v;
+    }
+  }
+};
+
+// Tile (tp, tq) and part of k of a workgroup.  Consecutive workgroups go to
+// the 8 XCDs in turn, each with an L2 of its own: every XCD gets a contiguous
+// run of tiles, and a run goes down groups of 8 q tiles, so that what is in
+// flight on one XCD shares rows of both operands.
+__device__ __forceinline__ void tile_of(int id, int total, int tps, int tqs, int* tp, int* tq, int* split) {
+  const int per = total / 8, over = total % 8, x = id % 8;
+  id = id / 8 + x * per + (x < over ? x : over);
+  const int tiles = tps * tqs;
+  *split = id / tiles;
+  id -= *split * tiles;
+  const int group = id / (8 * tps), first = group * 8;
+  const int size = tqs - first < 8 ? tqs - first : 8;
+  id -= group * 8 * tps;
+  *tq = first + id % size;
+  *tp = id / size;
+}
+
+// WP x WQ outputs per wave.  kGated: the rows of a wave's P tile are WP / 2
+// gate rows and their up rows, so that a lane has both sums of a column.
+template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int EPI, bool GATED>
+__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(const Prod a, const Epi e) {
+  constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
+  static_assert(!GATED || !PS, "the gated layer's weights are read along k");
+  typedef Operand<T, PS, BP, NW> OP;
+  typedef Operand<T, QS, BQ, NW> OQ;
+  __shared__ __align__(16) char p0[OP::kBytes], p1[OP::kBytes], q0[OQ::kBytes], q1[OQ::kBytes];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wp = wave % NWP, wq = wave / NWP;
+  constexpr int BC = GATED ? BP / 2 : BP;  // result columns of a tile
+  const int tps = (a.np + BC - 1) / BC, tqs = (a.nq + BQ - 1) / BQ;
+  int tp, tq, split;
+  tile_of(blockIdx.x, gridDim.x, tps, tqs, &tp, &tq, &split);
+  const int cp = tp * BC, cq = tq * BQ;
+  const int step0 = split * a.steps;
+  const int all = (a.nk * (int)sizeof(T) + 127) / 128;
+  const int nsteps = min(a.steps, all - step0);
+
+  // Where each load of this wave starts (bytes from the tile's first byte).
+  int vp[OP::kLoads], vq[OQ::kLoads];
+#pragma unroll
+  for (int j = 0; j < OP::kLoads; ++j) {
+    int r = OP::lds_row(wave, lane, j);
+    if (GATED) r = (r / WP) * (WP / 2) + r % (WP / 2);
+    vp[j] = (int)(r * a.ldp) + OP::chunk(wave, lane, j) * 16;
+  }
+#pragma unroll
+  for (int j = 0; j < OQ::kLoads; ++j)
+    vq[j] = (int)(OQ::lds_row(wave, lane, j) * a.ldq) + OQ::chunk(wave, lane, j) * 16;
+  const char* bp = a.p + (PS ? (long long)cp * (int)sizeof(T) : cp * a.ldp);
+  const char* bq = a.q + (QS ? (long long)cq * (int)sizeof(T) : cq * a.ldq);
+  const long long kbytes = (long long)a.nk * (int)sizeof(T);
+
+  auto stage = [&](int step, char* lp, char* lq) {
+    // C: bytes of k before this step; S: rows of k before it.
+    const long long at = (long long)step * 128, row = (long long)step * OP::kStep;
+    const bool tail = at + 128 > kbytes;
+    const long long op = PS ? row * a.ldp : at, oq = QS ? row * a.ldq : at;
+    const long long ep = PS ? (a.kp - 1 - row) * a.ldp + (long long)(a.colsp - cp) * (int)sizeof(T)
+                            : (a.np - 1 - cp) * a.ldp + kbytes - at;
+    const long long eq = QS ? (a.kq - 1 - row) * a.ldq + (long long)(a.colsq - cq) * (int)sizeof(T)
+                            : (a.nq - 1 - cq) * a.ldq + kbytes - at;
+    const __amdgpu_buffer_rsrc_t rq = descriptor(bq + oq, eq), rp = descriptor(bp + op, ep);
+    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(bp + op + a.p2 * a.ldp, ep) : rp;
+#pragma unroll
+    for (int j = 0; j < OP::kLoads; ++j) {
+      int v = vp[j];
+      if (!PS && tail && at + OP::chunk(wave, lane, j) * 16 >= kbytes) v = (int)0x80000000;
+      const bool up = GATED && ((wave + j * NW) * OP::kRowsPer) % WP >= WP / 2;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(up ? rp2 : rp, (lds_void*)(lp + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < OQ::kLoads; ++j) {
+      int v = vq[j];
+      if (!QS && tail && at + OQ::chunk(wave, lane, j) * 16 >= kbytes) v = (int)0x80000000;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lq + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
+    }
+  };
+
+  f4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+  auto compute = [&](const char* lp, const char* lq) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      typename Num<T>::Frag fp[FP], fq[FQ];
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) fq[j] = OQ::frag(lq, lane, wq * WQ, j, kk);
+#pragma unroll
+      for (int i = 0; i < FP; ++i) fp[i] = OP::frag(lp, lane, wp * WP, i, kk);
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(fp[i], fq[j], acc[i][j]);
+    }
+  };
+  // This wave's loads have landed and its reads are done; then everyone's.
+  auto sync = [] {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  stage(step0, p0, q0);
+  for (int s = 0; s < nsteps; s += 2) {
+    sync();
+    if (s + 1 < nsteps) stage(step0 + s + 1, p1, q1);
+    compute(p0, q0);
+    if (s + 1 < nsteps) {
+      sync();
+      if (s + 2 < nsteps) stage(step0 + s + 2, p0, q0);
+      compute(p1, q1);
+    }
+  }
+
+  // ---- epilogue: acc[i][j] holds p = 16 i + 4 g + 0..3 of q = 16 j + lane % 16
+  const int g = lane >> 4, c = lane & 15;
+  const int q_first = cq + wq * WQ + c;
+  if constexpr (EPI == kStats) {
+    const int p_first = cp + wp * WP + 4 * g;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int q = q_first + 16 * j;
+      const long long label = q < a.nq ? e.labels[q] - e.class0 : -1;
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+        const int p = p_first + 16 * i;
+        const f4 z = class_logits<T>(e, a.np, p, acc[i][j]);
+        acc[i][j] = z;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          m = fmaxf(m, z[n]);
+          if (label == p + n && p + n < a.np) e.zlabel[q] = z[n];
+        }
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum += acc[i][j][n] == -INFINITY ? 0.f : __expf(acc[i][j][n] - m);
+      float2 t = make_float2(m, sum);
+#pragma unroll
+      for (int o = 16; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));
+      if (g == 0 && q < a.nq) e.stat[(long long)(tp * NWP + wp) * a.nq + q] = t;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int q = q_first + 16 * j;
+      if (q >= a.nq) continue;
+      if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < FP / 2; ++i) {
+          const int p = cp + wp * (WP / 2) + 16 * i + 4 * g;
+          if constexpr (EPI == kPartial) {
+            if (p < a.np) {
+              float* t = a.part + ((long long)split * a.nq + q) * a.ldpart + p;
+              *reinterpret_cast<f4*>(t) = acc[i][j];
+              *reinterpret_cast<f4*>(t + a.ldpart / 2) = acc[i + FP / 2][j];
+            }
+          } else {
+            emit_gated<T>(e, a.np, q, p, acc[i][j], acc[i + FP / 2][j]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+          const int p = cp + wp * WP + 16 * i + 4 * g;
+          if constexpr (EPI == kPartial) {
+            if (p < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + p) = acc[i][j];
+          } else if constexpr (EPI == kXgrad) {
+            if (p < e.ldy) emit_xgrad<T>(e, a.np, q, p, acc[i][j]);
+          } else {
+            emit_linear<T>(e, a.np, q, p, acc[i][j]);
+          }
+        }
+      }
+    }
+  }
+}
+
+}  // namespace dense
+}  // namespace qcnn

@@ -1,0 +1,617 @@
+// The dense layers for one element type: planning, the kernels around the
+// products, and the calls of qcnn_internal.h.  Included once per type
+// (dense_f32.hip, dense_bf16.hip, dense_f16.hip).
+#pragma once
+
+#include "dense_core.h"
+
+namespace qcnn {
+namespace dense {
+
+inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+// Parts of one call's workspace.
+struct Layout {
+  size_t bytes = 0;
+  size_t add(size_t b) {
+    const size_t at = bytes;
+    bytes += align256(b);
+    return at;
+  }
+};
+
+template <typename T>
+constexpr int pad16(int n) {  // elements, to whole 16 bytes
+  constexpr int u = 16 / (int)sizeof(T);
+  return (n + u - 1) / u * u;
+}
+
+template <typename T>
+bool wide(const void* p, long long ld, int cols) {  // rows of whole aligned 16 bytes
+  constexpr int u = 16 / (int)sizeof(T);
+  return ((uintptr_t)p & 15) == 0 && ld % u == 0 && cols % u == 0;
+}
+
+template <typename T>
+bool quads(const void* p, long long ld) {
+  return p == nullptr || (((uintptr_t)p & (4 * sizeof(T) - 1)) == 0 && ld % 4 == 0);
+}
+
+// ------------------------------------------------------ kernels around them
+
+// [rows][cols] with row stride ld -> rows of ldo, zeros past cols.
+template <typename T>
+__global__ __launch_bounds__(256) void pad_kernel(const T* __restrict__ src, long long ld, int rows, int cols,
+                                                  T* __restrict__ dst, int ldo) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= ldo) return;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) dst[(long long)r * ldo + c] = c < cols ? src[r * ld + c] : (T)0.f;
+}
+
+// dz = dy act'(pre) (kGated: gate and up halves) and its sums over rows.
+// A thread has 4 columns and goes down `chunk` rows; the sums of a block's
+// rows go to part[blockIdx.y][columns of dz], joined by colsum_kernel: the
+// order of the additions is the same in every run.
+struct Slope {
+  const void* dy;
+  const void* pre;
+  void* dz;     // null: only the sums
+  float* part;  // null: no sums
+  long long lddy, ldpre, lddz;
+  int rows, cols, chunk, act, vec;  // cols: of dy; vec: dy, pre, dz take quads
+};
+
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
+  const int p = (blockIdx.x * 256 + threadIdx.x) * 4;
+  const long long width = GATED ? 2 * a.cols : a.cols;
+  if (p >= a.cols) {
+    // the zeros between the columns and the row's end
+    if (a.dz && p < a.cols + 32) {
+      const long long col = width + (p - (a.cols + 3) / 4 * 4);
+      for (int r = blockIdx.y * a.chunk; r < min(a.rows, (blockIdx.y + 1) * a.chunk); ++r)
+        for (int i = 0; i < 4; ++i)
+          if (col + i < a.lddz) static_cast<T*>(a.dz)[r * a.lddz + col + i] = (T)0.f;
+    }
+    return;
+  }
+  const int n = a.cols - p;
+  const bool full = a.vec && n >= 4;
+  f4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+  for (int r = blockIdx.y * a.chunk; r < min(a.rows, (blockIdx.y + 1) * a.chunk); ++r) {
+    const f4 dy = load_quad(static_cast<const T*>(a.dy) + r * a.lddy + p, full, n);
+    if constexpr (GATED) {
+      const T* z = static_cast<const T*>(a.pre) + r * a.ldpre + p;
+      const f4 g = load_quad(z, full, n), u = load_quad(z + a.cols, full, n);
+      f4 dg, du;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dg[i] = dy[i] * u[i] * act_slope<T>(a.act, g[i]);
+        du[i] = dy[i] * act_value<T>(a.act, g[i]);
+      }
+      T* o = static_cast<T*>(a.dz) + r * a.lddz + p;
+      store_quad(o, dg, full, n);
+      store_quad(o + a.cols, du, full, n);
+      s0 += dg;
+      s1 += du;
+    } else {
+      f4 d = dy;
+      if (a.act != QCNN_ACT_NONE) {
+        const f4 z = load_quad(static_cast<const T*>(a.pre) + r * a.ldpre + p, full, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] *= act_slope<T>(a.act, z[i]);
+      }
+      if (a.dz) store_quad(static_cast<T*>(a.dz) + r * a.lddz + p, d, full, n);
+      s0 += d;
+    }
+  }
+  if (a.part) {
+    float* o = a.part + blockIdx.y * width + p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) {
+        o[i] = s0[i];
+        if (GATED) o[a.cols + i] = s1[i];
+      }
+  }
+}
+
+// out[c] = alpha sum_r part[r][c]
+template <typename T>
+__global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ part, int rows, long long width,
+                                                     const float* alpha, T* __restrict__ out) {
+  const long long c = blockIdx.x * 256LL + threadIdx.x;
+  if (c >= width) return;
+  float s = 0.f;
+  for (int r = 0; r < rows; ++r) s += part[r * width + c];
+  out[c] = (T)(alpha ? s * *alpha : s);
+}
+
+// Sums of the parts of k, then the epilogue: a thread per quad of a row.
+template <typename T, int EPI>
+__global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ part, int splits, long long ldpart,
+                                                     int np, int nq, int quads_of_row, const Epi e) {
+  const long long id = blockIdx.x * 256LL + threadIdx.x;
+  const int q = (int)(id / quads_of_row), p = (int)(id % quads_of_row) * 4;
+  if (q >= nq) return;
+  const long long each = (long long)nq * ldpart;
+  const float* s = part + q * ldpart + p;
+  f4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
+  if (p < np)
+    for (int i = 0; i < splits; ++i) {
+      v += *reinterpret_cast<const f4*>(s + i * each);
+      if (EPI == kGated) u += *reinterpret_cast<const f4*>(s + i * each + ldpart / 2);
+    }
+  if constexpr (EPI == kGated) emit_gated<T>(e, np, q, p, v, u);
+  else if constexpr (EPI == kXgrad) emit_xgrad<T>(e, np, q, p, v);
+  else emit_linear<T>(e, np, q, p, v);
+}
+
+// The same for the loss: a wave per row and 256 classes.
+template <typename T>
+__global__ __launch_bounds__(256) void finish_stats_kernel(const float* __restrict__ part, int splits,
+                                                           long long ldpart, int np, int nq, int slots, const Epi e) {
+  const long long id = blockIdx.x * 4LL + (threadIdx.x >> 6);
+  const int q = (int)(id % nq), slot = (int)(id / nq), lane = threadIdx.x & 63, p = slot * 256 + lane * 4;
+  if (slot >= slots) return;
+  f4 z = {0.f, 0.f, 0.f, 0.f};
+  if (p < np)
+    for (int i = 0; i < splits; ++i)
+      z += *reinterpret_cast<const f4*>(part + ((long long)i * nq + q) * ldpart + p);
+  z = class_logits<T>(e, np, p, z);
+  const long long label = e.labels[q] - e.class0;
+  float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (label == p + i && p + i < np) e.zlabel[q] = z[i];
+    sum += z[i] == -INFINITY ? 0.f : __expf(z[i] - m);
+  }
+  float2 t = make_float2(m, sum);
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));
+  if (lane == 0) e.stat[(long long)slot * nq + q] = t;
+}
+
+// Joins the slots' maxima and sums of each row: 16 rows by 16 groups of slots.
+static __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ stat, const float* __restrict__ zlabel,
+                                                   const long long* __restrict__ labels, int slots, int nq,
+                                                   int classes, float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float2 part[16][16];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, q = blockIdx.x * 16 + c;
+  float2 t = make_float2(-INFINITY, 0.f);
+  if (q < nq)
+    for (int s = r; s < slots; s += 16) t = join_stat(t, stat[(long long)s * nq + q]);
+  part[r][c] = t;
+  __syncthreads();
+  if (r != 0 || q >= nq) return;
+  for (int i = 1; i < 16; ++i) t = join_stat(t, part[i][c]);
+  const float l = t.x + logf(t.y);
+  const long long label = labels[q];
+  lse[q] = l;
+  loss[q] = label < 0 ? 0.f : label >= classes ? NAN : l - zlabel[q];
+}
+
+// out[0] = the largest finite |dloss| of a counted row (1 if there is none or
+// it is 0), out[1] = out[0] / gain: what products with d are multiplied by.
+static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restrict__ dloss,
+                                                    const long long* __restrict__ labels, int n, float gain,
+                                                    float* __restrict__ out) {
+  __shared__ float part[16];
+  float m = 0.f;
+  for (int i = threadIdx.x; i < n; i += 1024) {
+    const float v = fabsf(dloss[i]);
+    if (labels[i] >= 0 && v < INFINITY) m = fmaxf(m, v);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
+  if (m == 0.f) m = 1.f;
+  out[0] = m;
+  out[1] = m / gain;
+}
+
+// ---------------------------------------------------------------- planning
+
+// A product's tiles and parts of k.  256 CUs: fewer tiles than that are split
+// along k, as long as a part keeps 4 steps to cover its first loads.
+struct Cut {
+  int splits, steps;
+  size_t part_bytes;
+  long long ldpart;
+};
+
+template <typename T>
+Cut cut_of(int np, int nq, int nk, bool gated) {
+  const long long tiles = (long long)ceil_div(np, gated ? 64 : 128) * ceil_div(nq, 128);
+  const int all = ceil_div(nk * (int)sizeof(T), 128);
+  int splits = tiles >= 192 ? 1 : (int)std::min<long long>(256 / tiles, all / 4);
+  if (splits < 1) splits = 1;
+  Cut c;
+  c.steps = ceil_div(all, splits);
+  c.splits = ceil_div(all, c.steps);
+  c.ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
+  c.part_bytes = c.splits > 1 ? (size_t)c.splits * nq * c.ldpart * 4 : 0;
+  return c;
+}
+
+template <typename T, bool PS, bool QS, int EPI, bool GATED>
+hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStream_t st) {
+  a.splits = c.splits;
+  a.steps = c.steps;
+  a.part = part;
+  a.ldpart = c.ldpart;
+  const int tiles = ceil_div(a.np, GATED ? 64 : 128) * ceil_div(a.nq, 128);
+  const dim3 grid(tiles * c.splits), block(256);
+  LaunchTimer timer;
+  hipError_t err;
+  if (c.splits == 1)
+    return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, EPI, GATED>, grid, block, 0u, st, a, e);
+  err = timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, kPartial, GATED>, grid, block, 0u, st, a, e);
+  if (err != hipSuccess) return err;
+  if constexpr (EPI == kStats) {
+    const int slots = ceil_div(a.np, 256);
+    const long long waves = (long long)slots * a.nq;
+    finish_stats_kernel<T><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(part, c.splits, c.ldpart, a.np, a.nq, slots, e);
+  } else {
+    const int per = EPI == kXgrad ? (int)(e.ldy / 4) : ceil_div(a.np, 4);
+    const long long n = (long long)per * a.nq;
+    finish_kernel<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, c.splits, c.ldpart, a.np, a.nq, per, e);
+  }
+  return hipGetLastError();
+}
+
+// Slots of kStats: one per wave along p, or per 256 classes after a split.
+template <typename T>
+int stat_slots(const Cut& c, int np) { return c.splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, 128); }
+
+// A matrix as the products read it: the caller's, or a copy with padded rows.
+template <typename T>
+struct Source {
+  const T* p;
+  long long ld;
+  int rows, cols;
+  bool copy;
+  size_t at = 0;
+  Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l)
+      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(!wide<T>(ptr, ld_, cols_)) {
+    if (copy) at = l->add((size_t)rows * pad16<T>(cols) * sizeof(T));
+  }
+  hipError_t place(char* ws, hipStream_t st) {
+    if (!copy) return hipSuccess;
+    T* o = reinterpret_cast<T*>(ws + at);
+    const int ldo = pad16<T>(cols);
+    pad_kernel<T><<<dim3(ceil_div(ldo, 256), std::min(rows, 4096)), 256, 0, st>>>(p, ld, rows, cols, o, ldo);
+    p = o;
+    ld = ldo;
+    return hipGetLastError();
+  }
+  long long bytes() const { return ld * (long long)sizeof(T); }
+  const char* ptr() const { return reinterpret_cast<const char*>(p); }
+};
+
+template <typename T>
+Prod forward_prod(const Source<T>& w, const Source<T>& x, int np) {
+  Prod a = {};
+  a.p = w.ptr();
+  a.q = x.ptr();
+  a.ldp = w.bytes();
+  a.ldq = x.bytes();
+  a.np = np;
+  a.nq = x.rows;
+  a.nk = pad16<T>(x.cols);
+  a.p2 = np;
+  return a;
+}
+
+// ------------------------------------------------------------------- calls
+
+// The call's workspace: the caller's or the stream's.  `*asked`: the caller
+// only wants its size.
+inline hipError_t claim(Scratch* ws, const Layout& l, const Room& room, hipStream_t st, bool* asked) {
+  *asked = room.bytes && !room.ptr;
+  if (*asked) {
+    *room.bytes = l.bytes;
+    return hipSuccess;
+  }
+  if (l.bytes == 0) return hipSuccess;
+  const Workspace own{static_cast<char*>(room.ptr), room.bytes ? *room.bytes : 0};
+  return ws->take(st, l.bytes, room.ptr ? &own : nullptr);
+}
+
+template <typename T>
+hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, const void* bias, int act,
+                          const void* res, void* pre, void* y, const Room& room, hipStream_t st) {
+  Layout l;
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
+  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), false);
+  const size_t part = l.add(c.part_bytes);
+  Scratch ws;
+  bool asked;
+  hipError_t e = claim(&ws, l, room, st, &asked);
+  if (asked) return e;
+  if (e == hipSuccess) e = xs.place(ws.get(), st);
+  if (e == hipSuccess) e = wsrc.place(ws.get(), st);
+  if (e != hipSuccess) return e;
+  Epi p = {};
+  p.y = y;
+  p.ldy = s.ldy;
+  p.pre = pre;
+  p.ldpre = s.Ct;
+  p.bias = bias;
+  p.res = res;
+  p.ldr = s.ldr;
+  p.act = act;
+  p.vec = quads<T>(y, s.ldy) && quads<T>(pre, s.Ct) && quads<T>(bias, 4) && quads<T>(res, s.ldr);
+  return run_product<T, false, false, kLinear, false>(forward_prod(wsrc, xs, s.Ct), p, c,
+                                                      reinterpret_cast<float*>(ws.get() + part), st);
+}
+
+template <typename T>
+hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, const void* bias, int act, void* pre,
+                         void* y, const Room& room, hipStream_t st) {
+  Layout l;
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, 2 * s.Ct, s.Cs, &l);
+  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), true);
+  const size_t part = l.add(c.part_bytes);
+  Scratch ws;
+  bool asked;
+  hipError_t e = claim(&ws, l, room, st, &asked);
+  if (asked) return e;
+  if (e == hipSuccess) e = xs.place(ws.get(), st);
+  if (e == hipSuccess) e = wsrc.place(ws.get(), st);
+  if (e != hipSuccess) return e;
+  Epi p = {};
+  p.y = y;
+  p.ldy = s.ldy;
+  p.pre = pre;
+  p.ldpre = 2LL * s.Ct;
+  p.bias = bias;
+  p.act = act;
+  p.vec = s.Ct % 4 == 0 && quads<T>(y, s.ldy) && quads<T>(pre, 4) && quads<T>(bias, 4);
+  return run_product<T, false, false, kGated, true>(forward_prod(wsrc, xs, s.Ct), p, c,
+                                                    reinterpret_cast<float*>(ws.get() + part), st);
+}
+
+constexpr int kChunkRows = 64;  // rows whose bias gradients one thread adds up
+
+// dx = dz w, as fp32 running sums in `acc` or finished in y.
+template <typename T>
+Prod dx_prod(const Source<T>& w, const char* wp, int wrows, const char* dz, long long lddz, int N) {
+  Prod a = {};
+  a.p = wp;
+  a.ldp = w.bytes();
+  a.np = w.cols;
+  a.colsp = pad16<T>(w.cols);
+  a.kp = wrows;
+  a.q = dz;
+  a.ldq = lddz * (long long)sizeof(T);
+  a.nq = N;
+  a.nk = pad16<T>(wrows);
+  return a;
+}
+
+// dw = dz^T x
+template <typename T>
+Prod dw_prod(const Source<T>& x, const char* dz, long long lddz, int wrows) {
+  Prod a = {};
+  a.p = x.ptr();
+  a.ldp = x.bytes();
+  a.np = x.cols;
+  a.colsp = pad16<T>(x.cols);
+  a.kp = x.rows;
+  a.q = dz;
+  a.ldq = lddz * (long long)sizeof(T);
+  a.nq = wrows;
+  a.colsq = pad16<T>(wrows);
+  a.kq = x.rows;
+  a.nk = x.rows;
+  return a;
+}
+
+// Both layers' gradients from dz: rows of the weight `rows` (2 C_t if gated).
+template <typename T, bool GATED>
+hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, const void* w, const void* pre, int act,
+                          void* dx, void* dw, void* dbias, const Room& room, hipStream_t st) {
+  const int rows = GATED ? 2 * s.Ct : s.Ct;
+  Layout l;
+  // With no activation dy is dz, where the products can read it in place.
+  const bool in_place = !GATED && act == QCNN_ACT_NONE && (wide<T>(dy, s.ldy, s.Ct) || (!dx && !dw));
+  const long long lddz = in_place ? s.ldy : pad16<T>(rows);
+  const size_t dz_at = in_place ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
+  const int chunks = ceil_div(s.N, kChunkRows);
+  const size_t sums_at = dbias ? l.add((size_t)chunks * rows * 4) : 0;
+  Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
+  const Cut cx = cut_of<T>(s.Cs, s.N, pad16<T>(rows), false), cw = cut_of<T>(s.Cs, rows, s.N, false);
+  const size_t part = l.add(std::max(dx ? cx.part_bytes : 0, dw ? cw.part_bytes : 0));
+  Scratch ws;
+  bool asked;
+  hipError_t e = claim(&ws, l, room, st, &asked);
+  if (asked) return e;
+  if (e == hipSuccess && dw) e = xs.place(ws.get(), st);
+  if (e == hipSuccess && dx) e = wsrc.place(ws.get(), st);
+  if (e != hipSuccess) return e;
+  const char* dz = in_place ? static_cast<const char*>(dy) : ws.get() + dz_at;
+  if (!in_place || dbias) {
+    Slope a = {};
+    a.dy = dy;
+    a.pre = pre;
+    a.dz = in_place ? nullptr : ws.get() + dz_at;
+    a.part = dbias ? reinterpret_cast<float*>(ws.get() + sums_at) : nullptr;
+    a.lddy = s.ldy;
+    a.ldpre = rows;
+    a.lddz = lddz;
+    a.rows = s.N;
+    a.cols = s.Ct;
+    a.chunk = kChunkRows;
+    a.act = act;
+    a.vec = quads<T>(dy, s.ldy) && quads<T>(pre, 4) && (!GATED ? quads<T>(pre, rows) : s.Ct % 4 == 0);
+    const int threads = ceil_div(s.Ct, 4) + (in_place ? 0 : 4);
+    slope_kernel<T, GATED><<<dim3(ceil_div(threads, 256), chunks), 256, 0, st>>>(a);
+    e = hipGetLastError();
+    if (e == hipSuccess && dbias) {
+      colsum_kernel<T><<<ceil_div(rows, 256), 256, 0, st>>>(a.part, chunks, rows, nullptr, static_cast<T*>(dbias));
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+  }
+  float* sums = reinterpret_cast<float*>(ws.get() + part);
+  if (dx) {
+    Epi p = {};
+    p.y = dx;
+    p.ldy = s.Cs;
+    p.vec = quads<T>(dx, s.Cs);
+    e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr(), rows, dz, lddz, s.N), p, cx, sums, st);
+    if (e != hipSuccess) return e;
+  }
+  if (dw) {
+    Epi p = {};
+    p.y = dw;
+    p.ldy = s.Cs;
+    p.vec = quads<T>(dw, s.Cs);
+    e = run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, rows), p, cw, sums, st);
+  }
+  return e;
+}
+
+template <typename T>
+hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, const void* bias, const long long* labels,
+                        float* loss, float* lse, const Room& room, hipStream_t st) {
+  Layout l;
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
+  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), false);
+  const int slots = stat_slots<T>(c, s.Ct);
+  const size_t part = l.add(c.part_bytes), stat = l.add((size_t)slots * s.N * 8), zl = l.add((size_t)s.N * 4);
+  Scratch ws;
+  bool asked;
+  hipError_t e = claim(&ws, l, room, st, &asked);
+  if (asked) return e;
+  if (e == hipSuccess) e = xs.place(ws.get(), st);
+  if (e == hipSuccess) e = wsrc.place(ws.get(), st);
+  if (e != hipSuccess) return e;
+  Epi p = {};
+  p.bias = bias;
+  p.vec = quads<T>(bias, 4);
+  p.labels = labels;
+  p.stat = reinterpret_cast<float2*>(ws.get() + stat);
+  p.zlabel = reinterpret_cast<float*>(ws.get() + zl);
+  p.classes = s.Ct;
+  e = run_product<T, false, false, kStats, false>(forward_prod(wsrc, xs, s.Ct), p, c,
+                                                  reinterpret_cast<float*>(ws.get() + part), st);
+  if (e != hipSuccess) return e;
+  loss_kernel<<<ceil_div(s.N, 16), 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
+  return hipGetLastError();
+}
+
+// Bytes of the logits' gradient that are held at once.
+constexpr size_t kPieceBytes = (size_t)256 << 20;
+
+template <typename T>
+hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, const void* bias, const long long* labels,
+                         const float* lse, const float* dloss, void* dx, void* dw, void* dbias, const Room& room, hipStream_t st) {
+  Layout l;
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
+  long long fit = (long long)(kPieceBytes / ((size_t)s.N * sizeof(T))) / 256 * 256;
+  if (fit < 256) fit = 256;
+  const int piece = fit < s.Ct ? (int)fit : s.Ct, pieces = ceil_div(s.Ct, piece);
+  const long long ldd = pad16<T>(piece), ldacc = (s.Cs + 3) / 4 * 4;
+  const size_t d_at = l.add((size_t)s.N * ldd * sizeof(T)), scale_at = l.add(8);
+  const size_t acc_at = dx && pieces > 1 ? l.add((size_t)s.N * ldacc * 4) : 0;
+  const int chunks = ceil_div(s.N, kChunkRows);
+  const size_t sums_at = dbias ? l.add((size_t)chunks * piece * 4) : 0;
+  size_t part_bytes = 0;
+  for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
+    part_bytes = std::max(part_bytes, cut_of<T>(n, s.N, pad16<T>(s.Cs), false).part_bytes);
+    if (dx) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, s.N, pad16<T>(n), false).part_bytes);
+    if (dw) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, n, s.N, false).part_bytes);
+  }
+  const size_t part = l.add(part_bytes);
+  Scratch ws;
+  bool asked;
+  hipError_t e = claim(&ws, l, room, st, &asked);
+  if (asked) return e;
+  if (e == hipSuccess) e = xs.place(ws.get(), st);
+  if (e == hipSuccess) e = wsrc.place(ws.get(), st);
+  if (e != hipSuccess) return e;
+  float* scale = reinterpret_cast<float*>(ws.get() + scale_at);
+  float* sums = reinterpret_cast<float*>(ws.get() + part);
+  char* d = ws.get() + d_at;
+  const float gain = sizeof(T) == 2 && (float)(T)1e-7f == 1.1920929e-07f ? 1024.f : 1.f;  // fp16: 2^10
+  dmax_kernel<<<1, 1024, 0, st>>>(dloss, labels, s.N, gain, scale);
+  e = hipGetLastError();
+  for (int k = 0; k < pieces && e == hipSuccess; ++k) {
+    const int c0 = k * piece, n = std::min(piece, s.Ct - c0);
+    const long long ld = pad16<T>(n);
+    Epi p = {};
+    p.y = d;
+    p.ldy = ld;
+    p.bias = bias;
+    p.vec = quads<T>(bias, 4);
+    p.labels = labels;
+    p.lse = lse;
+    p.dloss = dloss;
+    p.dmax = scale;
+    p.gain = gain;
+    p.class0 = c0;
+    p.classes = s.Ct;
+    Prod a = forward_prod(wsrc, xs, n);
+    a.p += c0 * wsrc.bytes();
+    e = run_product<T, false, false, kXgrad, false>(a, p, cut_of<T>(n, s.N, pad16<T>(s.Cs), false), sums, st);
+    if (e == hipSuccess && dbias) {
+      Slope b = {};
+      b.dy = d;
+      b.lddy = ld;
+      b.part = reinterpret_cast<float*>(ws.get() + sums_at);
+      b.rows = s.N;
+      b.cols = n;
+      b.chunk = kChunkRows;
+      b.act = QCNN_ACT_NONE;
+      b.vec = 1;
+      slope_kernel<T, false><<<dim3(ceil_div(ceil_div(n, 4), 256), chunks), 256, 0, st>>>(b);
+      colsum_kernel<T><<<ceil_div(n, 256), 256, 0, st>>>(b.part, chunks, n, scale + 1, static_cast<T*>(dbias) + c0);
+      e = hipGetLastError();
+    }
+    if (e == hipSuccess && dx) {
+      Epi o = {};
+      o.y = dx;
+      o.ldy = s.Cs;
+      o.vec = quads<T>(dx, s.Cs);
+      o.alpha = scale + 1;
+      o.acc = reinterpret_cast<float*>(ws.get() + acc_at);
+      o.ldacc = ldacc;
+      o.acc_in = k > 0;
+      o.acc_out = k + 1 < pieces;
+      e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr() + c0 * wsrc.bytes(), n, d, ld, s.N), o,
+                                                      cut_of<T>(s.Cs, s.N, pad16<T>(n), false), sums, st);
+    }
+    if (e == hipSuccess && dw) {
+      Epi o = {};
+      o.y = static_cast<T*>(dw) + (long long)c0 * s.Cs;
+      o.ldy = s.Cs;
+      o.vec = quads<T>(o.y, s.Cs);
+      o.alpha = scale + 1;
+      e = run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, n), o, cut_of<T>(s.Cs, n, s.N, false), sums,
+                                                     st);
+    }
+  }
+  return e;
+}
+
+template <typename T>
+hipError_t dispatch(const DenseCall& c, hipStream_t st) {
+  switch (c.op) {
+    case kLinearForward: return linear_forward<T>(c.s, c.x, c.w, c.bias, c.act, c.res, const_cast<void*>(c.pre), c.y, c.room, st);
+    case kGatedForward: return gated_forward<T>(c.s, c.x, c.w, c.bias, c.act, const_cast<void*>(c.pre), c.y, c.room, st);
+    case kLinearBackward: return layer_backward<T, false>(c.s, c.dy, c.x, c.w, c.pre, c.act, c.dx, c.dw, c.dbias, c.room, st);
+    case kGatedBackward: return layer_backward<T, true>(c.s, c.dy, c.x, c.w, c.pre, c.act, c.dx, c.dw, c.dbias, c.room, st);
+    case kXentForward: return xent_forward<T>(c.s, c.x, c.w, c.bias, c.labels, c.loss, c.lse, c.room, st);
+    case kXentBackward:
+      return xent_backward<T>(c.s, c.x, c.w, c.bias, c.labels, c.lse, static_cast<const float*>(c.dy), c.dx, c.dw, c.dbias, c.room, st);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace dense
+}  // namespace qcnn

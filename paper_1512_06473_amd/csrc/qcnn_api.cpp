@@ -226,7 +226,7 @@ const char* qcnn_status_string(qcnn_status s) {
     case QCNN_ERR_HIP: return "HIP runtime error";
     case QCNN_ERR_UNSUPPORTED: return "layer not supported by the kernels (C's > 16, grid or LDS limits)";
     case QCNN_ERR_ALIAS: return "an output overlaps an input";
-    case QCNN_ERR_WORKSPACE: return "the layer needs more scratch than qcnn_conv_forward_noalloc holds";
+    case QCNN_ERR_WORKSPACE: return "the layer needs more scratch than qcnn_conv_forward_noalloc holds or the caller gave";
   }
   return "unknown status";
 }

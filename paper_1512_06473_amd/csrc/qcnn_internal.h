@@ -320,6 +320,42 @@ hipError_t launch_ec_conv(int N, int Cs, int H, int W, int Ct, int dk, int strid
                           const float* S, const float* T, float* D, uint8_t* codes, int sweeps, int inner,
                           double* objective, hipStream_t stream);
 
+// Dense fully-connected layers (dense_f32.hip, dense_bf16.hip, dense_f16.hip;
+// the checks are in dense_api.cpp).
+namespace dense {
+
+struct LinearShape {
+  int N, Cs, Ct;
+  long long ldx, ldy, ldr;  // row strides in elements; ldy: of y or dy
+};
+
+// The caller's workspace: ptr and its size, or, with ptr null, where to write
+// the size that the call needs (nothing is launched); both null: the stream's.
+struct Room {
+  void* ptr;
+  size_t* bytes;
+};
+
+enum Op { kLinearForward, kLinearBackward, kGatedForward, kGatedBackward, kXentForward, kXentBackward };
+
+struct DenseCall {
+  Op op;
+  LinearShape s;
+  int act;
+  const void *x, *w, *bias, *res, *dy;  // dy of kXentBackward: dloss
+  const void* pre;                      // written by the forward calls
+  void *y, *dx, *dw, *dbias;
+  const long long* labels;
+  float *loss, *lse;
+  Room room;
+};
+
+hipError_t run_f32(const DenseCall& c, hipStream_t stream);
+hipError_t run_bf16(const DenseCall& c, hipStream_t stream);
+hipError_t run_f16(const DenseCall& c, hipStream_t stream);
+
+}  // namespace dense
+
 // The library's own stream-ordered memory pool on the current device
 // (scratch.cpp): created on first use, it keeps freed memory for reuse (its
 // release threshold is unlimited) and leaves the device's default pool, and
