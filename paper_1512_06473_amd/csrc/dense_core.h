@@ -25,6 +25,8 @@
 // not stored.
 #pragma once
 
+#include <type_traits>
+
 #include "qcnn_internal.h"
 
 namespace qcnn {
@@ -299,42 +301,46 @@ struct Operand {
   static constexpr int kRowsPer = 64 / kPerRow;            // LDS rows of one wave's load
   static constexpr int kLoads = ROWS * 128 / 1024 / NW;    // loads of one wave and step
   static constexpr int kBytes = ROWS * 128;
+  static constexpr int kReads = S ? (kS == 2 ? 2 : 4) : 1;  // LDS reads of a fragment
   static_assert(kLoads >= 1 && kLoads * NW * 1024 == ROWS * 128, "whole loads");
   static_assert(!S || kRowBytes >= 256, "the swizzle of S tiles spans 256 bytes");
   static_assert(kPerRow <= 64, "a row per load at least");
 
   // XOR on the chunk index of LDS row r.
-  static __device__ __forceinline__ int swizzle(int r) {
-    if (!S) return (r >> 1) & 7;
-    if (kS == 2) return 2 * ((r & 3) | (((r >> 3) & 1) << 2));
-    return 4 * ((r >> 2) & 3);
+  static constexpr __host__ __device__ int swizzle(int r) {
+    return !S ? (r >> 1) & 7 : kS == 2 ? 2 * ((r & 3) | (((r >> 3) & 1) << 2)) : 4 * ((r >> 2) & 3);
   }
 
-  // Offset of lane's 16 bytes of load j from the tile's first byte in memory.
-  // LDS row r is the operand's row r (gated: see row_of in the kernel).
-  static __device__ __forceinline__ int lds_row(int wave, int lane, int j) {
-    return (wave + j * NW) * kRowsPer + lane / kPerRow;
+  // Load j of a wave fills kRowsPer LDS rows from first(j); a lane's row among
+  // them and its chunk there (in bytes; the first load's, the others differ by
+  // a constant) do not depend on j.
+  static __device__ __forceinline__ int first(int wave, int j) { return (wave + j * NW) * kRowsPer; }
+  static __device__ __forceinline__ int lane_row(int lane) { return lane / kPerRow; }
+  static __device__ __forceinline__ int lane_chunk(int wave, int lane) {
+    return ((lane % kPerRow) ^ swizzle(first(wave, 0) + lane_row(lane))) * 16;
   }
-  static __device__ __forceinline__ int chunk(int wave, int lane, int j) {
-    return (lane % kPerRow) ^ swizzle(lds_row(wave, lane, j));
-  }
+  static constexpr __device__ int chunk_delta(int j) { return swizzle(j * NW * kRowsPer) * 16; }
 
-  // Fragment f (16 rows from row `at` + 16 f) of the kk-th part of a step.
-  static __device__ __forceinline__ typename Num<T>::Frag frag(const char* lds, int lane, int at, int f, int kk) {
+  // Where a lane reads its part of the fragments of rows at, at + 1, ...
+  static __device__ __forceinline__ int lane_base(int lane, int at) {
     const int g = lane >> 4, i = lane & 15;
+    if (!S) return (at + i) * 128 + ((g ^ (i >> 1)) << 4);
+    if (kS == 2)
+      return (8 * g + (i >> 2)) * kRowBytes + (((at >> 3) + ((i & 3) >> 1)) ^ (2 * ((i >> 2) | ((g & 1) << 2)))) * 16 +
+             (i & 1) * 8;
+    return 4 * g * kRowBytes + (((at + i) >> 2) ^ (4 * g)) * 16 + (i & 3) * 4;
+  }
+
+  // Fragment f (16 rows further on each) of the kk-th part of a step.
+  static __device__ __forceinline__ typename Num<T>::Frag frag(const char* lds, int base, int f, int kk) {
     if constexpr (!S) {
-      const int r = at + f * 16 + i;
-      return *reinterpret_cast<const typename Num<T>::Frag*>(lds + r * 128 + (((kk * 4 + g) ^ (i >> 1)) << 4));
+      return *reinterpret_cast<const typename Num<T>::Frag*>(lds + (base ^ (kk * 64)) + f * 2048);
     } else if constexpr (kS == 2) {
-      const int k = kk * 32 + 8 * g + (i >> 2);
-      const int c = (((at + f * 16) >> 3) + ((i & 3) >> 1)) ^ (2 * ((i >> 2) | ((g & 1) << 2)));
-      const char* a = lds + k * kRowBytes + c * 16 + (i & 1) * 8;
+      const char* a = lds + (base ^ (f * 32)) + kk * 32 * kRowBytes;
       const auto lo = Num<T>::read_tr(a), hi = Num<T>::read_tr(a + 4 * kRowBytes);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      const int k = kk * 16 + 4 * g;
-      const int col = at + f * 16 + i;
-      const char* a = lds + k * kRowBytes + ((col >> 2) ^ (4 * g)) * 16 + (col & 3) * 4;
+      const char* a = lds + (base ^ (f * 64)) + kk * 16 * kRowBytes;
       f4 v;
 #pragma unroll
       for (int n = 0; n < 4; ++n) v[n] = *reinterpret_cast<const float*>(a + n * kRowBytes);
@@ -342,6 +348,16 @@ struct Operand {
     }
   }
 };
+
+// This wave's loads but the last N have landed and its LDS reads are done;
+// then everyone's.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // Tile (tp, tq) and part of k of a workgroup.  Consecutive workgroups go to
 // the 8 XCDs in turn, each with an L2 of its own: every XCD gets a contiguous
@@ -381,43 +397,39 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   const int all = (a.nk * (int)sizeof(T) + 127) / 128;
   const int nsteps = min(a.steps, all - step0);
 
-  // Where each load of this wave starts (bytes from the tile's first byte).
-  int vp[OP::kLoads], vq[OQ::kLoads];
-#pragma unroll
-  for (int j = 0; j < OP::kLoads; ++j) {
-    int r = OP::lds_row(wave, lane, j);
-    if (GATED) r = (r / WP) * (WP / 2) + r % (WP / 2);
-    vp[j] = (int)(r * a.ldp) + OP::chunk(wave, lane, j) * 16;
-  }
-#pragma unroll
-  for (int j = 0; j < OQ::kLoads; ++j)
-    vq[j] = (int)(OQ::lds_row(wave, lane, j) * a.ldq) + OQ::chunk(wave, lane, j) * 16;
+  // What a lane adds to the first byte of each load's first row.
+  const int lp_ = (int)(OP::lane_row(lane) * a.ldp), cp_ = OP::lane_chunk(wave, lane);
+  const int lq_ = (int)(OQ::lane_row(lane) * a.ldq), cq_ = OQ::lane_chunk(wave, lane);
   const char* bp = a.p + (PS ? (long long)cp * (int)sizeof(T) : cp * a.ldp);
   const char* bq = a.q + (QS ? (long long)cq * (int)sizeof(T) : cq * a.ldq);
   const long long kbytes = (long long)a.nk * (int)sizeof(T);
 
-  auto stage = [&](int step, char* lp, char* lq) {
+  auto stage = [&](int s, char* lp, char* lq) {
     // C: bytes of k before this step; S: rows of k before it.
+    const int step = step0 + s;
+    const bool none = s >= nsteps;  // loads nothing: the loop runs ahead of its end
     const long long at = (long long)step * 128, row = (long long)step * OP::kStep;
-    const bool tail = at + 128 > kbytes;
+    const int left = (int)min(kbytes - at, 128LL);  // C: bytes of k in this step
     const long long op = PS ? row * a.ldp : at, oq = QS ? row * a.ldq : at;
     const long long ep = PS ? (a.kp - 1 - row) * a.ldp + (long long)(a.colsp - cp) * (int)sizeof(T)
                             : (a.np - 1 - cp) * a.ldp + kbytes - at;
     const long long eq = QS ? (a.kq - 1 - row) * a.ldq + (long long)(a.colsq - cq) * (int)sizeof(T)
                             : (a.nq - 1 - cq) * a.ldq + kbytes - at;
-    const __amdgpu_buffer_rsrc_t rq = descriptor(bq + oq, eq), rp = descriptor(bp + op, ep);
-    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(bp + op + a.p2 * a.ldp, ep) : rp;
+    const __amdgpu_buffer_rsrc_t rq = descriptor(bq + oq, none ? 0 : eq), rp = descriptor(bp + op, none ? 0 : ep);
+    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(bp + op + a.p2 * a.ldp, none ? 0 : ep) : rp;
 #pragma unroll
     for (int j = 0; j < OP::kLoads; ++j) {
-      int v = vp[j];
-      if (!PS && tail && at + OP::chunk(wave, lane, j) * 16 >= kbytes) v = (int)0x80000000;
-      const bool up = GATED && ((wave + j * NW) * OP::kRowsPer) % WP >= WP / 2;
+      int r = OP::first(wave, j);
+      const bool up = GATED && r % WP >= WP / 2;
+      if (GATED) r = r / WP * (WP / 2) + r % (WP / 2);
+      int v = lp_ + (cp_ ^ OP::chunk_delta(j)) + (int)(r * a.ldp);
+      if (!PS) v = cp_ >= left ? (int)0x80000000 : v;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(up ? rp2 : rp, (lds_void*)(lp + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
     }
 #pragma unroll
     for (int j = 0; j < OQ::kLoads; ++j) {
-      int v = vq[j];
-      if (!QS && tail && at + OQ::chunk(wave, lane, j) * 16 >= kbytes) v = (int)0x80000000;
+      int v = lq_ + (cq_ ^ OQ::chunk_delta(j)) + (int)(OQ::first(wave, j) * a.ldq);
+      if (!QS) v = cq_ >= left ? (int)0x80000000 : v;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lq + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
     }
   };
@@ -428,39 +440,74 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
 #pragma unroll
     for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
-  auto compute = [&](const char* lp, const char* lq) {
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      typename Num<T>::Frag fp[FP], fq[FQ];
-#pragma unroll
-      for (int j = 0; j < FQ; ++j) fq[j] = OQ::frag(lq, lane, wq * WQ, j, kk);
-#pragma unroll
-      for (int i = 0; i < FP; ++i) fp[i] = OP::frag(lp, lane, wp * WP, i, kk);
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(fp[i], fq[j], acc[i][j]);
-    }
+  struct Frags {
+    typename Num<T>::Frag p[FP], q[FQ];
   };
-  // This wave's loads have landed and its reads are done; then everyone's.
-  auto sync = [] {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+  int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
+  auto read = [&](Frags& f, const char* lp, const char* lq, int kk) {
+    // One register each: the fragments' addresses are made from it again
+    // every time (the registers are for the sums and two sets of fragments).
+    asm volatile("" : "+v"(rp_), "+v"(rq_));
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) f.q[j] = OQ::frag(lq, rq_, j, kk);
+#pragma unroll
+    for (int i = 0; i < FP; ++i) f.p[i] = OP::frag(lp, rp_, i, kk);
+  };
+  auto multiply = [&](const Frags& f) {
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
+  };
+  // LDS reads, and a step's loads, one by one between the products.
+  auto interleave = [](auto loads_) {
+    constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ * (sizeof(T) == 4 ? 4 : 1);
+    constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
+    constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      if (i < reads) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+      }
+      if (i < loads) {
+        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+      }
+    }
+    constexpr int rest = mmas - per * (reads + loads);
+    if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
+  };
+  // A step: the first half's fragments are in f0.  Reads its second half
+  // under the first half's products; then everyone's reads of this buffer are
+  // done and everyone's loads of the other have landed: the step after the
+  // next is sent for, and the next step's first half is read under the second
+  // half's products.
+  Frags f0, f1;
+  auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) {
+    read(f1, lp, lq, 1);
+    multiply(f0);
+    interleave(std::integral_constant<int, 0>());
+    __builtin_amdgcn_sched_barrier(0);
+    wait_and_meet<0>();
+    stage(s + 2, lp, lq);
+    read(f0, next_p, next_q, 0);
+    multiply(f1);
+    interleave(std::integral_constant<int, OP::kLoads + OQ::kLoads>());
+    __builtin_amdgcn_sched_barrier(0);
   };
 
-  stage(step0, p0, q0);
-  for (int s = 0; s < nsteps; s += 2) {
-    sync();
-    if (s + 1 < nsteps) stage(step0 + s + 1, p1, q1);
-    compute(p0, q0);
-    if (s + 1 < nsteps) {
-      sync();
-      if (s + 2 < nsteps) stage(step0 + s + 2, p0, q0);
-      compute(p1, q1);
-    }
+  stage(0, p0, q0);
+  stage(1, p1, q1);
+  wait_and_meet<OP::kLoads + OQ::kLoads>();
+  read(f0, p0, q0, 0);
+  int s = 0;
+  for (; s + 2 <= nsteps; s += 2) {
+    body(s, p0, q0, p1, q1);
+    body(s + 1, p1, q1, p0, q0);
   }
+  if (s < nsteps) body(s, p0, q0, p1, q1);
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing is on its way to this LDS any more
 
   // ---- epilogue: acc[i][j] holds p = 16 i + 4 g + 0..3 of q = 16 j + lane % 16
   const int g = lane >> 4, c = lane & 15;

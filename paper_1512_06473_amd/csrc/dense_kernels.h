@@ -3,6 +3,7 @@
 // (dense_f32.hip, dense_bf16.hip, dense_f16.hip).
 #pragma once
 
+#include <stdlib.h>
 #include "dense_core.h"
 
 namespace qcnn {
@@ -218,18 +219,29 @@ static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restri
 // A product's tiles and parts of k.  256 CUs: fewer tiles than that are split
 // along k, as long as a part keeps 4 steps to cover its first loads.
 struct Cut {
+  int big;  // 256 x 256 tiles of 8 waves, else 128 x 128 of 4
   int splits, steps;
   size_t part_bytes;
   long long ldpart;
 };
 
+inline long long tiles_of(int np, int nq, bool gated, int edge) {
+  return (long long)ceil_div(np, gated ? edge / 2 : edge) * ceil_div(nq, edge);
+}
+
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated) {
-  const long long tiles = (long long)ceil_div(np, gated ? 64 : 128) * ceil_div(nq, 128);
+  const long long small = tiles_of(np, nq, gated, 128), large = tiles_of(np, nq, gated, 256);
   const int all = ceil_div(nk * (int)sizeof(T), 128);
+  Cut c;
+  // Rounds of the chip times the work of a tile: a CU holds one large tile or
+  // two small ones at a time, and a large one moves half the LDS bytes per
+  // product.
+  const long long t_large = (large + 255) / 256 * 4 * 16, t_small = (small + 511) / 512 * 2 * 21;
+  c.big = getenv("QBIG") ? atoi(getenv("QBIG")) : t_large <= t_small;
+  const long long tiles = c.big ? large : small;
   int splits = tiles >= 192 ? 1 : (int)std::min<long long>(256 / tiles, all / 4);
   if (splits < 1) splits = 1;
-  Cut c;
   c.steps = ceil_div(all, splits);
   c.splits = ceil_div(all, c.steps);
   c.ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
@@ -238,18 +250,22 @@ Cut cut_of(int np, int nq, int nk, bool gated) {
 }
 
 template <typename T, bool PS, bool QS, int EPI, bool GATED>
+hipError_t launch_product(const Prod& a, const Epi& e, const Cut& c, hipStream_t st) {
+  LaunchTimer timer;
+  const dim3 grid((unsigned)tiles_of(a.np, a.nq, GATED, c.big ? 256 : 128) * c.splits);
+  if (c.big)
+    return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
+  return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+}
+
+template <typename T, bool PS, bool QS, int EPI, bool GATED>
 hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStream_t st) {
   a.splits = c.splits;
   a.steps = c.steps;
   a.part = part;
   a.ldpart = c.ldpart;
-  const int tiles = ceil_div(a.np, GATED ? 64 : 128) * ceil_div(a.nq, 128);
-  const dim3 grid(tiles * c.splits), block(256);
-  LaunchTimer timer;
-  hipError_t err;
-  if (c.splits == 1)
-    return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, EPI, GATED>, grid, block, 0u, st, a, e);
-  err = timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, kPartial, GATED>, grid, block, 0u, st, a, e);
+  if (c.splits == 1) return launch_product<T, PS, QS, EPI, GATED>(a, e, c, st);
+  const hipError_t err = launch_product<T, PS, QS, kPartial, GATED>(a, e, c, st);
   if (err != hipSuccess) return err;
   if constexpr (EPI == kStats) {
     const int slots = ceil_div(a.np, 256);
@@ -263,9 +279,11 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   return hipGetLastError();
 }
 
-// Slots of kStats: one per wave along p, or per 256 classes after a split.
-template <typename T>
-int stat_slots(const Cut& c, int np) { return c.splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, 128); }
+// Slots of kStats: one per wave along p (2 in a tile), or per 256 classes
+// after a split.
+inline int stat_slots(const Cut& c, int np) {
+  return c.splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, c.big ? 256 : 128);
+}
 
 // A matrix as the products read it: the caller's, or a copy with padded rows.
 template <typename T>
@@ -482,7 +500,7 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   Layout l;
   Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
   const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), false);
-  const int slots = stat_slots<T>(c, s.Ct);
+  const int slots = stat_slots(c, s.Ct);
   const size_t part = l.add(c.part_bytes), stat = l.add((size_t)slots * s.N * 8), zl = l.add((size_t)s.N * 4);
   Scratch ws;
   bool asked;
