@@ -507,12 +507,12 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
     body(s + 1, p1, q1, p0, q0);
   }
   if (s < nsteps) body(s, p0, q0, p1, q1);
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing is on its way to this LDS any more
+  wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
 
   // ---- epilogue: acc[i][j] holds p = 16 i + 4 g + 0..3 of q = 16 j + lane % 16
   const int g = lane >> 4, c = lane & 15;
-  const int q_first = cq + wq * WQ + c;
   if constexpr (EPI == kStats) {
+    const int q_first = cq + wq * WQ + c;
     const int p_first = cp + wp * WP + 4 * g;
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
@@ -541,35 +541,48 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
       if (g == 0 && q < a.nq) e.stat[(long long)(tp * NWP + wp) * a.nq + q] = t;
     }
   } else {
+    // Through LDS, a wave's 16 KB of it: 64 lanes in the products' order hold
+    // 16 rows' 32 bytes each, and memory wants whole lines (stored as they
+    // are, 2.4 times the result's bytes were written to HBM).  Row q's quad p
+    // lies at p ^ (q % 16), free of conflicts both ways.
+    constexpr int kRoom = 4 * OP::kBytes / NW, kRows = kRoom / (WP * 4) < WQ ? kRoom / (WP * 4) : WQ;
+    constexpr int kQuads = WP / 4, kOut = GATED ? kQuads / 2 : kQuads;  // of a row; that one emit covers
+    static_assert(OP::kBytes == OQ::kBytes && OP::kBytes % kRoom == 0, "a wave's room lies in one tile");
+    constexpr int kPer = OP::kBytes / kRoom;
+    char* const tiles[4] = {p0, p1, q0, q1};
+    f4* room = reinterpret_cast<f4*>(tiles[0] + wave % kPer * kRoom);
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int q = q_first + 16 * j;
-      if (q >= a.nq) continue;
-      if constexpr (GATED) {
+    for (int t = 1; t < 4; ++t)
+      if (wave / kPer == t) room = reinterpret_cast<f4*>(tiles[t] + wave % kPer * kRoom);
 #pragma unroll
-        for (int i = 0; i < FP / 2; ++i) {
-          const int p = cp + wp * (WP / 2) + 16 * i + 4 * g;
+    for (int first = 0; first < WQ; first += kRows) {
+#pragma unroll
+      for (int j = 0; j < kRows / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < FP; ++i) room[(16 * j + c) * kQuads + ((4 * i + g) ^ c)] = acc[i][first / 16 + j];
+#pragma unroll 4
+      for (int t = 0; t < kRows * kOut / 64; ++t) {
+        const int row = t * (64 / kOut) + lane / kOut, quad = lane % kOut;
+        const int q = cq + wq * WQ + first + row, p = cp + wp * (GATED ? WP / 2 : WP) + 4 * quad;
+        const f4 v = room[row * kQuads + (quad ^ (row & 15))];
+        if (q >= a.nq) continue;
+        if constexpr (GATED) {
+          const f4 u = room[row * kQuads + ((quad + kOut) ^ (row & 15))];
           if constexpr (EPI == kPartial) {
             if (p < a.np) {
-              float* t = a.part + ((long long)split * a.nq + q) * a.ldpart + p;
-              *reinterpret_cast<f4*>(t) = acc[i][j];
-              *reinterpret_cast<f4*>(t + a.ldpart / 2) = acc[i + FP / 2][j];
+              float* o = a.part + ((long long)split * a.nq + q) * a.ldpart + p;
+              *reinterpret_cast<f4*>(o) = v;
+              *reinterpret_cast<f4*>(o + a.ldpart / 2) = u;
             }
           } else {
-            emit_gated<T>(e, a.np, q, p, acc[i][j], acc[i + FP / 2][j]);
+            emit_gated<T>(e, a.np, q, p, v, u);
           }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < FP; ++i) {
-          const int p = cp + wp * WP + 16 * i + 4 * g;
-          if constexpr (EPI == kPartial) {
-            if (p < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + p) = acc[i][j];
-          } else if constexpr (EPI == kXgrad) {
-            if (p < e.ldy) emit_xgrad<T>(e, a.np, q, p, acc[i][j]);
-          } else {
-            emit_linear<T>(e, a.np, q, p, acc[i][j]);
-          }
+        } else if constexpr (EPI == kPartial) {
+          if (p < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + p) = v;
+        } else if constexpr (EPI == kXgrad) {
+          if (p < e.ldy) emit_xgrad<T>(e, a.np, q, p, v);
+        } else {
+          emit_linear<T>(e, a.np, q, p, v);
         }
       }
     }
