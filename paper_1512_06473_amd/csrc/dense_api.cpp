@@ -65,10 +65,6 @@ qcnn_status run(int dtype, DenseCall& c, void* workspace, size_t* workspace_byte
   c.room = qcnn::dense::Room{workspace, workspace_bytes};
   const hipStream_t st = (hipStream_t)stream;
   try {
-    if (!workspace_bytes) {
-      hipMemPool_t pool = nullptr;
-      if (qcnn::library_pool(&pool) != hipSuccess) return QCNN_ERR_HIP;
-    }
     const hipError_t e = dtype == QCNN_F32 ? qcnn::dense::run_f32(c, st)
                          : dtype == QCNN_BF16 ? qcnn::dense::run_bf16(c, st)
                                               : qcnn::dense::run_f16(c, st);

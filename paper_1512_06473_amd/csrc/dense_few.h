@@ -1,0 +1,185 @@
+// Forward products of few rows: y[q][p] = sum_k w[p][k] x[q][k], q < 32.
+//
+// Every weight is used for a handful of products only, so the time is that of
+// reading w once, and what matters is how many bytes are on their way.  The
+// MFMA operand layout (lane (g, i): row i, 16 bytes at k chunk g) is also a
+// good order of reading a row-major matrix: a wave's 16-byte loads take 64
+// bytes of 16 rows, kBatch loads in a row 64 kBatch bytes of each.  So w goes
+// from memory to the matrix cores' registers, without LDS; x comes the same
+// way, out of L2.  A workgroup's 8 waves share groups of 16 p and parts of k:
+// with `ks` parts, 8 / ks groups; the parts meet in LDS.  Rows may start at any
+// element: the loads are unaligned where they have to be.
+#pragma once
+
+#include "dense_core.h"
+
+namespace qcnn {
+namespace dense {
+
+struct Few {
+  const char* p;        // w
+  const char* q;        // x
+  long long ldp, ldq;   // bytes
+  int np, nq, nk;       // nk: elements, any number
+  int p2;               // gated: rows from a gate row to its up row
+  int ks, units;        // parts of k in a workgroup; 64-byte units of k in each part
+  int splits;           // workgroups along k
+  float* part;
+  long long ldpart;
+};
+
+constexpr int kFewWaves = 8, kBatch = 8;
+
+template <typename T>
+__device__ __forceinline__ typename Num<T>::Frag load_any(const char* p) {
+  typename Num<T>::Frag v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+// FP times 16 weight rows per wave (gated: half of them the gate's, the others
+// their up projections).
+template <typename T, int FP, int FQ, int EPI, bool GATED>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(const Few a, const Epi e) {
+  constexpr int kUnit = 64 / (int)sizeof(T), kPer = 16 / (int)sizeof(T);  // k's of a unit, of a lane's load
+  __shared__ f4 parts[kFewWaves][FP * FQ][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15;
+  const int groups = kFewWaves / a.ks, kpart = wave % a.ks;
+  constexpr int kCols = GATED ? 8 * FP : 16 * FP;  // result columns of a group
+  const int tp = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const int p_first = (tp * groups + wave / a.ks) * kCols;
+  const int units = (a.nk + kUnit - 1) / kUnit;
+  const int u0 = min(units, (split * a.ks + kpart) * a.units), u1 = min(units, u0 + a.units);
+
+  f4 acc[FP][FQ];
+#pragma unroll
+  for (int f = 0; f < FP; ++f)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[f][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+  if (p_first < a.np) {
+    // Rows past the end read the last one's; what they add up to is not stored.
+    const char *rp[FP], *rq[FQ];
+#pragma unroll
+    for (int f = 0; f < FP; ++f) {
+      const long long row = min(p_first + 16 * (GATED ? f % (FP / 2) : f) + i, a.np - 1) + (GATED && f >= FP / 2 ? a.p2 : 0);
+      rp[f] = a.p + row * a.ldp + g * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) rq[j] = a.q + (long long)min(16 * j + i, a.nq - 1) * a.ldq + g * 16;
+
+    const int full = min(u1, a.nk / kUnit);  // units that end within the row
+    int u = u0;
+    for (; u + kBatch <= full; u += kBatch) {
+      typename Num<T>::Frag vp[kBatch][FP], vq[kBatch][FQ];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const long long at = (long long)(u + b) * 64;
+#pragma unroll
+        for (int f = 0; f < FP; ++f) vp[b][f] = load_any<T>(rp[f] + at);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) vq[b][j] = load_any<T>(rq[j] + at);
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) acc[f][j] = Num<T>::mma(vp[b][f], vq[b][j], acc[f][j]);
+    }
+    for (; u < u1; ++u) {
+      typename Num<T>::Frag vp[FP], vq[FQ];
+      const int n = a.nk - u * kUnit - g * kPer;  // k's left for this lane
+#pragma unroll
+      for (int f = 0; f < FP + FQ; ++f) {
+        const char* r = (f < FP ? rp[f < FP ? f : 0] : rq[f < FP ? 0 : f - FP]) + (long long)u * 64;
+        typename Num<T>::Frag v;
+        if (n >= kPer) {
+          v = load_any<T>(r);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) {
+            T t = (T)0.f;
+            if (k < n) t = reinterpret_cast<const T*>(r)[k];
+            v[k] = t;
+          }
+        }
+        if (f < FP) vp[f < FP ? f : 0] = v;
+        else vq[f < FP ? 0 : f - FP] = v;
+      }
+#pragma unroll
+      for (int f = 0; f < FP; ++f)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[f][j] = Num<T>::mma(vp[f], vq[j], acc[f][j]);
+    }
+  }
+
+  // Parts of k meet; the first wave of each group goes on.
+  if (a.ks > 1) {
+#pragma unroll
+    for (int f = 0; f < FP; ++f)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) parts[wave][f * FQ + j][lane] = acc[f][j];
+    __syncthreads();
+    if (kpart == 0)
+      for (int w = 1; w < a.ks; ++w)
+#pragma unroll
+        for (int f = 0; f < FP; ++f)
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) acc[f][j] += parts[wave + w][f * FQ + j][lane];
+  }
+  if (kpart != 0 || p_first >= a.np) return;
+  const int p = p_first + 4 * g;
+#pragma unroll
+  for (int j = 0; j < FQ; ++j) {
+    const int q = 16 * j + i;
+    if constexpr (EPI == kStats) {
+      const long long label = q < a.nq ? e.labels[q] - e.class0 : -1;
+      float2 t = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int f = 0; f < FP; ++f) {
+        const f4 z = class_logits<T>(e, a.np, p + 16 * f, acc[f][j]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          if (label == p + 16 * f + n && p + 16 * f + n < a.np) e.zlabel[q] = z[n];
+          t = join_stat(t, make_float2(z[n], z[n] == -INFINITY ? 0.f : z[n] != z[n] ? z[n] : 1.f));
+        }
+      }
+#pragma unroll
+      for (int o = 16; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));
+      if (g == 0 && q < a.nq) e.stat[(long long)(p_first / kCols) * a.nq + q] = t;
+    } else {
+      if (q >= a.nq) continue;
+      if constexpr (GATED) {
+#pragma unroll
+        for (int f = 0; f < FP / 2; ++f) {
+          const int pf = p + 16 * f;
+          if constexpr (EPI == kPartial) {
+            if (pf < a.np) {
+              float* o = a.part + ((long long)split * a.nq + q) * a.ldpart + pf;
+              *reinterpret_cast<f4*>(o) = acc[f][j];
+              *reinterpret_cast<f4*>(o + a.ldpart / 2) = acc[f + FP / 2][j];
+            }
+          } else {
+            emit_gated<T>(e, a.np, q, pf, acc[f][j], acc[f + FP / 2][j]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < FP; ++f) {
+          const int pf = p + 16 * f;
+          if constexpr (EPI == kPartial) {
+            if (pf < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + pf) = acc[f][j];
+          } else if constexpr (EPI == kXgrad) {
+            if (pf < e.ldy) emit_xgrad<T>(e, a.np, q, pf, acc[f][j]);
+          } else {
+            emit_linear<T>(e, a.np, q, pf, acc[f][j]);
+          }
+        }
+      }
+    }
+  }
+}
+
+}  // namespace dense
+}  // namespace qcnn

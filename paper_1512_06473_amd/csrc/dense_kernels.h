@@ -3,8 +3,7 @@
 // (dense_f32.hip, dense_bf16.hip, dense_f16.hip).
 #pragma once
 
-#include <stdlib.h>
-#include "dense_core.h"
+#include "dense_few.h"
 
 namespace qcnn {
 namespace dense {
@@ -173,19 +172,29 @@ __global__ __launch_bounds__(256) void finish_stats_kernel(const float* __restri
   if (lane == 0) e.stat[(long long)slot * nq + q] = t;
 }
 
-// Joins the slots' maxima and sums of each row: 16 rows by 16 groups of slots.
-static __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ stat, const float* __restrict__ zlabel,
-                                                   const long long* __restrict__ labels, int slots, int nq,
-                                                   int classes, float* __restrict__ loss, float* __restrict__ lse) {
-  __shared__ float2 part[16][16];
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, q = blockIdx.x * 16 + c;
+// Joins the slots' maxima and sums of each row: ROWS rows by 256 / ROWS
+// threads, each of which takes every so many-th slot.
+template <int ROWS>
+static __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ stat,
+                                                          const float* __restrict__ zlabel,
+                                                          const long long* __restrict__ labels, int slots, int nq,
+                                                          int classes, float* __restrict__ loss,
+                                                          float* __restrict__ lse) {
+  constexpr int kEach = 256 / ROWS;
+  __shared__ float2 part[kEach][ROWS];
+  const int c = threadIdx.x % ROWS, r = threadIdx.x / ROWS, q = blockIdx.x * ROWS + c;
   float2 t = make_float2(-INFINITY, 0.f);
-  if (q < nq)
-    for (int s = r; s < slots; s += 16) t = join_stat(t, stat[(long long)s * nq + q]);
+  if (q < nq) {
+#pragma unroll 4
+    for (int s = r; s < slots; s += kEach) t = join_stat(t, stat[(long long)s * nq + q]);
+  }
   part[r][c] = t;
-  __syncthreads();
+  for (int n = kEach / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (r < n) part[r][c] = join_stat(part[r][c], part[r + n][c]);
+  }
   if (r != 0 || q >= nq) return;
-  for (int i = 1; i < 16; ++i) t = join_stat(t, part[i][c]);
+  t = part[0][c];
   const float l = t.x + logf(t.y);
   const long long label = labels[q];
   lse[q] = l;
@@ -238,7 +247,7 @@ Cut cut_of(int np, int nq, int nk, bool gated) {
   // two small ones at a time, and a large one moves half the LDS bytes per
   // product.
   const long long t_large = (large + 255) / 256 * 4 * 16, t_small = (small + 511) / 512 * 2 * 21;
-  c.big = getenv("QBIG") ? atoi(getenv("QBIG")) : t_large <= t_small;
+  c.big = t_large <= t_small;
   const long long tiles = c.big ? large : small;
   int splits = tiles >= 192 ? 1 : (int)std::min<long long>(256 / tiles, all / 4);
   if (splits < 1) splits = 1;
@@ -258,6 +267,21 @@ hipError_t launch_product(const Prod& a, const Epi& e, const Cut& c, hipStream_t
   return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
 }
 
+// After kPartial: the parts' sums and the epilogue.
+template <typename T, int EPI>
+hipError_t finish(int np, int nq, const Epi& e, const Cut& c, const float* part, hipStream_t st) {
+  if constexpr (EPI == kStats) {
+    const int slots = ceil_div(np, 256);
+    const long long waves = (long long)slots * nq;
+    finish_stats_kernel<T><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, slots, e);
+  } else {
+    const int per = EPI == kXgrad ? (int)(e.ldy / 4) : ceil_div(np, 4);
+    const long long n = (long long)per * nq;
+    finish_kernel<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, per, e);
+  }
+  return hipGetLastError();
+}
+
 template <typename T, bool PS, bool QS, int EPI, bool GATED>
 hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStream_t st) {
   a.splits = c.splits;
@@ -266,24 +290,79 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   a.ldpart = c.ldpart;
   if (c.splits == 1) return launch_product<T, PS, QS, EPI, GATED>(a, e, c, st);
   const hipError_t err = launch_product<T, PS, QS, kPartial, GATED>(a, e, c, st);
-  if (err != hipSuccess) return err;
-  if constexpr (EPI == kStats) {
-    const int slots = ceil_div(a.np, 256);
-    const long long waves = (long long)slots * a.nq;
-    finish_stats_kernel<T><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(part, c.splits, c.ldpart, a.np, a.nq, slots, e);
-  } else {
-    const int per = EPI == kXgrad ? (int)(e.ldy / 4) : ceil_div(a.np, 4);
-    const long long n = (long long)per * a.nq;
-    finish_kernel<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, c.splits, c.ldpart, a.np, a.nq, per, e);
-  }
-  return hipGetLastError();
+  return err != hipSuccess ? err : finish<T, EPI>(a.np, a.nq, e, c, part, st);
 }
 
-// Slots of kStats: one per wave along p (2 in a tile), or per 256 classes
-// after a split.
-inline int stat_slots(const Cut& c, int np) {
-  return c.splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, c.big ? 256 : 128);
-}
+// A forward product: the tiles, or for at most 32 rows the kernel that
+// streams the weights.
+constexpr int kFewRows = 32;
+
+template <typename T>
+struct Forward : Cut {
+  bool few, wide_ = false;
+  int ks, slots;  // slots: of kStats
+  int np, nq, nk;
+  bool gated;
+  Forward(int np_, int nq_, int nk_, bool gated_) : np(np_), nq(nq_), nk(nk_), gated(gated_) {
+    few = nq <= kFewRows;
+    if (!few) {
+      static_cast<Cut&>(*this) = cut_of<T>(np, nq, pad16<T>(nk), gated);
+      // one per wave along p (2 in a tile), or per 256 classes after a split
+      slots = splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, big ? 256 : 128);
+      return;
+    }
+    // A wave's 16 rows (32 past 8 rows of x and where there are many, whose
+    // loads of x then serve twice the weights: 50 against 55 us at 16 x 4096
+    // -> 22016) by 8192 waves' worth of parts of k within the workgroups:
+    // 4096 -> 22016 in bf16 took 53 us with 2048 waves, 38 with 4096, 37 with
+    // 8192.  A second kernel that joins workgroups costs 2 us: only for layers
+    // that would leave most CUs without a workgroup.
+    wide_ = !gated && (nq > 16 || (nq > 8 && np >= 16384));
+    const long long groups = ceil_div(np, cols());
+    const int all = ceil_div(nk * (int)sizeof(T), 64);
+    for (ks = 1; ks < kFewWaves && groups * ks < 8192 && all / (2 * ks) >= kBatch; ks *= 2) {}
+    int parts = groups * ks >= 2048 ? 1 : (int)std::min<long long>(4096 / (groups * ks), all / (ks * kBatch));
+    if (parts < 1) parts = 1;
+    steps = ceil_div(all, ks * parts);
+    splits = ceil_div(all, ks * steps);
+    ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
+    part_bytes = splits > 1 ? (size_t)splits * nq * ldpart * 4 : 0;
+    slots = splits > 1 ? ceil_div(np, 256) : ceil_div(np, cols());
+  }
+
+  int cols() const { return wide_ ? 32 : 16; }  // result columns of a wave
+
+  template <int EPI, bool GATED>
+  hipError_t launch_few(const Few& a, const Epi& e, hipStream_t st) const {
+    LaunchTimer timer;
+    const dim3 grid((unsigned)(ceil_div(ceil_div(np, cols()), kFewWaves / ks) * splits)), block(64 * kFewWaves);
+    if (nq > 16) return timed_launch(&timer, few_kernel<T, 2, 2, EPI, GATED>, grid, block, 0u, st, a, e);
+    if constexpr (!GATED)
+      if (!wide_) return timed_launch(&timer, few_kernel<T, 1, 1, EPI, GATED>, grid, block, 0u, st, a, e);
+    return timed_launch(&timer, few_kernel<T, 2, 1, EPI, GATED>, grid, block, 0u, st, a, e);
+  }
+
+  // w and x: rows of ldw and ldx bytes; as the tiles read them unless `few`.
+  template <int EPI, bool GATED>
+  hipError_t run(const char* w, long long ldw, const char* x, long long ldx, const Epi& e, float* part,
+                 hipStream_t st) const {
+    if (!few) {
+      Prod a = {};
+      a.p = w;
+      a.q = x;
+      a.ldp = ldw;
+      a.ldq = ldx;
+      a.np = a.p2 = np;
+      a.nq = nq;
+      a.nk = pad16<T>(nk);
+      return run_product<T, false, false, EPI, GATED>(a, e, *this, part, st);
+    }
+    Few a = {w, x, ldw, ldx, np, nq, nk, np, ks, steps, splits, part, ldpart};
+    if (splits == 1) return launch_few<EPI, GATED>(a, e, st);
+    const hipError_t err = launch_few<kPartial, GATED>(a, e, st);
+    return err != hipSuccess ? err : finish<T, EPI>(np, nq, e, *this, part, st);
+  }
+};
 
 // A matrix as the products read it: the caller's, or a copy with padded rows.
 template <typename T>
@@ -293,8 +372,8 @@ struct Source {
   int rows, cols;
   bool copy;
   size_t at = 0;
-  Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l)
-      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(!wide<T>(ptr, ld_, cols_)) {
+  Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l, bool tiles = true)
+      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(tiles && !wide<T>(ptr, ld_, cols_)) {
     if (copy) at = l->add((size_t)rows * pad16<T>(cols) * sizeof(T));
   }
   hipError_t place(char* ws, hipStream_t st) {
@@ -309,20 +388,6 @@ struct Source {
   long long bytes() const { return ld * (long long)sizeof(T); }
   const char* ptr() const { return reinterpret_cast<const char*>(p); }
 };
-
-template <typename T>
-Prod forward_prod(const Source<T>& w, const Source<T>& x, int np) {
-  Prod a = {};
-  a.p = w.ptr();
-  a.q = x.ptr();
-  a.ldp = w.bytes();
-  a.ldq = x.bytes();
-  a.np = np;
-  a.nq = x.rows;
-  a.nk = pad16<T>(x.cols);
-  a.p2 = np;
-  return a;
-}
 
 // ------------------------------------------------------------------- calls
 
@@ -343,8 +408,8 @@ template <typename T>
 hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, const void* bias, int act,
                           const void* res, void* pre, void* y, const Room& room, hipStream_t st) {
   Layout l;
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
-  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), false);
+  const Forward<T> c(s.Ct, s.N, s.Cs, false);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few);
   const size_t part = l.add(c.part_bytes);
   Scratch ws;
   bool asked;
@@ -363,7 +428,7 @@ hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, co
   p.ldr = s.ldr;
   p.act = act;
   p.vec = quads<T>(y, s.ldy) && quads<T>(pre, s.Ct) && quads<T>(bias, 4) && quads<T>(res, s.ldr);
-  return run_product<T, false, false, kLinear, false>(forward_prod(wsrc, xs, s.Ct), p, c,
+  return c.template run<kLinear, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                       reinterpret_cast<float*>(ws.get() + part), st);
 }
 
@@ -371,8 +436,8 @@ template <typename T>
 hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, const void* bias, int act, void* pre,
                          void* y, const Room& room, hipStream_t st) {
   Layout l;
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, 2 * s.Ct, s.Cs, &l);
-  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), true);
+  const Forward<T> c(s.Ct, s.N, s.Cs, true);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, 2 * s.Ct, s.Cs, &l, !c.few);
   const size_t part = l.add(c.part_bytes);
   Scratch ws;
   bool asked;
@@ -389,7 +454,7 @@ hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, con
   p.bias = bias;
   p.act = act;
   p.vec = s.Ct % 4 == 0 && quads<T>(y, s.ldy) && quads<T>(pre, 4) && quads<T>(bias, 4);
-  return run_product<T, false, false, kGated, true>(forward_prod(wsrc, xs, s.Ct), p, c,
+  return c.template run<kGated, true>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                     reinterpret_cast<float*>(ws.get() + part), st);
 }
 
@@ -498,9 +563,9 @@ template <typename T>
 hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, const void* bias, const long long* labels,
                         float* loss, float* lse, const Room& room, hipStream_t st) {
   Layout l;
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
-  const Cut c = cut_of<T>(s.Ct, s.N, pad16<T>(s.Cs), false);
-  const int slots = stat_slots(c, s.Ct);
+  const Forward<T> c(s.Ct, s.N, s.Cs, false);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few);
+  const int slots = c.slots;
   const size_t part = l.add(c.part_bytes), stat = l.add((size_t)slots * s.N * 8), zl = l.add((size_t)s.N * 4);
   Scratch ws;
   bool asked;
@@ -516,10 +581,15 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   p.stat = reinterpret_cast<float2*>(ws.get() + stat);
   p.zlabel = reinterpret_cast<float*>(ws.get() + zl);
   p.classes = s.Ct;
-  e = run_product<T, false, false, kStats, false>(forward_prod(wsrc, xs, s.Ct), p, c,
+  e = c.template run<kStats, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                   reinterpret_cast<float*>(ws.get() + part), st);
   if (e != hipSuccess) return e;
-  loss_kernel<<<ceil_div(s.N, 16), 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
+  // 16 rows read whole 128-byte lines; fewer than 64 rows would leave most of
+  // the chip idle and go down hundreds of slots one after another.
+  if (s.N >= 64)
+    loss_kernel<16><<<ceil_div(s.N, 16), 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
+  else
+    loss_kernel<1><<<s.N, 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
   return hipGetLastError();
 }
 
@@ -528,9 +598,11 @@ constexpr size_t kPieceBytes = (size_t)256 << 20;
 
 template <typename T>
 hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, const void* bias, const long long* labels,
-                         const float* lse, const float* dloss, void* dx, void* dw, void* dbias, const Room& room, hipStream_t st) {
+                         const float* lse, const float* dloss, void* dx, void* dw, void* dbias, const Room& room,
+                         hipStream_t st) {
   Layout l;
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l), wsrc(w, s.Cs, s.Ct, s.Cs, &l);
+  const bool few = s.N <= kFewRows;
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !few || dw), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !few || dx);
   long long fit = (long long)(kPieceBytes / ((size_t)s.N * sizeof(T))) / 256 * 256;
   if (fit < 256) fit = 256;
   const int piece = fit < s.Ct ? (int)fit : s.Ct, pieces = ceil_div(s.Ct, piece);
@@ -541,7 +613,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   const size_t sums_at = dbias ? l.add((size_t)chunks * piece * 4) : 0;
   size_t part_bytes = 0;
   for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
-    part_bytes = std::max(part_bytes, cut_of<T>(n, s.N, pad16<T>(s.Cs), false).part_bytes);
+    part_bytes = std::max(part_bytes, Forward<T>(n, s.N, s.Cs, false).part_bytes);
     if (dx) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, s.N, pad16<T>(n), false).part_bytes);
     if (dw) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, n, s.N, false).part_bytes);
   }
@@ -566,7 +638,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
     p.y = d;
     p.ldy = ld;
     p.bias = bias;
-    p.vec = quads<T>(bias, 4);
+    p.vec = quads<T>(bias, 4) && c0 % 4 == 0;
     p.labels = labels;
     p.lse = lse;
     p.dloss = dloss;
@@ -574,9 +646,8 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
     p.gain = gain;
     p.class0 = c0;
     p.classes = s.Ct;
-    Prod a = forward_prod(wsrc, xs, n);
-    a.p += c0 * wsrc.bytes();
-    e = run_product<T, false, false, kXgrad, false>(a, p, cut_of<T>(n, s.N, pad16<T>(s.Cs), false), sums, st);
+    e = Forward<T>(n, s.N, s.Cs, false).template run<kXgrad, false>(wsrc.ptr() + c0 * wsrc.bytes(), wsrc.bytes(),
+                                                                    xs.ptr(), xs.bytes(), p, sums, st);
     if (e == hipSuccess && dbias) {
       Slope b = {};
       b.dy = d;
