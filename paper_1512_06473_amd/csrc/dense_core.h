@@ -349,6 +349,38 @@ struct Operand {
   }
 };
 
+// Eight fp32 values as three bf16 parts each: the upper 8 bits of the 24, the
+// next 8, the last 8, each cut off (not rounded, so that nothing overflows),
+// which is exact.  Of the nine products of two numbers' parts the three
+// smallest, below 2^-22 of the whole, are left out.
+__device__ __forceinline__ void split_bf16(f4 a, f4 b, b8 (&out)[3]) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0 = i < 2 ? a[2 * i] : b[2 * i - 4], x1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
+      w[n][i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
+      x0 -= __uint_as_float(u0 & 0xffff0000u);
+      x1 -= __uint_as_float(u1 & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < 3; ++n) out[n] = __builtin_bit_cast(b8, w[n]);
+}
+
+// Whether any thread of the workgroup has `bad`; `word` is LDS that nobody uses.
+__device__ __forceinline__ bool any_of_group(bool bad, int* word) {
+  if (threadIdx.x == 0) *word = 0;
+  __syncthreads();
+  if (bad) *word = 1;
+  __syncthreads();
+  const bool any = *word != 0;
+  __syncthreads();
+  return any;
+}
+
 // This wave's loads but the last N have landed and its LDS reads are done;
 // then everyone's.
 template <int N>
@@ -404,7 +436,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   const char* bq = a.q + (QS ? (long long)cq * (int)sizeof(T) : cq * a.ldq);
   const long long kbytes = (long long)a.nk * (int)sizeof(T);
 
-  auto stage = [&](int s, char* lp, char* lq) {
+  auto stage = [&](int s, char* lp, char* lq) __attribute__((always_inline)) {
     // C: bytes of k before this step; S: rows of k before it.
     const int step = step0 + s;
     const bool none = s >= nsteps;  // loads nothing: the loop runs ahead of its end
@@ -440,74 +472,139 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
 #pragma unroll
     for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
-  struct Frags {
-    typename Num<T>::Frag p[FP], q[FQ];
-  };
-  int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
-  auto read = [&](Frags& f, const char* lp, const char* lq, int kk) {
-    // One register each: the fragments' addresses are made from it again
-    // every time (the registers are for the sums and two sets of fragments).
-    asm volatile("" : "+v"(rp_), "+v"(rq_));
+  if constexpr (sizeof(T) == 4) {
+    // fp32 as three bf16 parts (split_bf16): six products of them instead of
+    // fp32's own matrix instruction, which has 1/16 of bf16's rate.  The step's
+    // 32 k's are one bf16 instruction, elements 0..3 of a lane from its first
+    // half and 4..7 from its second.  An infinity's lower parts are NaN, so a
+    // tile whose sums are not all finite is computed again in fp32.
+    const int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
+    auto step = [&](const char* lp, const char* lq, auto split) __attribute__((always_inline)) {
+      if constexpr (decltype(split)::value) {
+        b8 fq[FQ][3];
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) f.q[j] = OQ::frag(lq, rq_, j, kk);
+        for (int j = 0; j < FQ; ++j) split_bf16(OQ::frag(lq, rq_, j, 0), OQ::frag(lq, rq_, j, 1), fq[j]);
 #pragma unroll
-    for (int i = 0; i < FP; ++i) f.p[i] = OP::frag(lp, rp_, i, kk);
-  };
-  auto multiply = [&](const Frags& f) {
+        for (int i = 0; i < FP; ++i) {
+          b8 fp[3];
+          split_bf16(OP::frag(lp, rp_, i, 0), OP::frag(lp, rp_, i, 1), fp);
+#pragma unroll
+          for (int n = 0; n < 6; ++n) {  // smallest first
+            constexpr int kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[kA[n]], fq[j][kB[n]], acc[i][j], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+              acc[i][j] = Num<T>::mma(OP::frag(lp, rp_, i, kk), OQ::frag(lq, rq_, j, kk), acc[i][j]);
+      }
+    };
+    auto loop = [&](auto split) __attribute__((always_inline)) {
+      stage(0, p0, q0);
+      for (int s = 0; s < nsteps; s += 2) {
+        wait_and_meet<0>();
+        stage(s + 1, p1, q1);
+        step(p0, q0, split);
+        if (s + 1 < nsteps) {
+          wait_and_meet<0>();
+          stage(s + 2, p0, q0);
+          step(p1, q1, split);
+        }
+      }
+      wait_and_meet<0>();
+    };
+    loop(std::true_type());
+    bool bad = false;
 #pragma unroll
     for (int i = 0; i < FP; ++i)
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
-  };
-  // LDS reads, and a step's loads, one by one between the products.
-  auto interleave = [](auto loads_) {
-    constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ * (sizeof(T) == 4 ? 4 : 1);
-    constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
-    constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
+      for (int j = 0; j < FQ; ++j)
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      if (i < reads) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-      }
-      if (i < loads) {
-        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-      }
+        for (int n = 0; n < 4; ++n) bad |= !(fabsf(acc[i][j][n]) < INFINITY);
+    if (any_of_group(bad, reinterpret_cast<int*>(p0))) {
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+      loop(std::false_type());
     }
-    constexpr int rest = mmas - per * (reads + loads);
-    if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
-  };
-  // A step: the first half's fragments are in f0.  Reads its second half
-  // under the first half's products; then everyone's reads of this buffer are
-  // done and everyone's loads of the other have landed: the step after the
-  // next is sent for, and the next step's first half is read under the second
-  // half's products.
-  Frags f0, f1;
-  auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) {
-    read(f1, lp, lq, 1);
-    multiply(f0);
-    interleave(std::integral_constant<int, 0>());
-    __builtin_amdgcn_sched_barrier(0);
-    wait_and_meet<0>();
-    stage(s + 2, lp, lq);
-    read(f0, next_p, next_q, 0);
-    multiply(f1);
-    interleave(std::integral_constant<int, OP::kLoads + OQ::kLoads>());
-    __builtin_amdgcn_sched_barrier(0);
-  };
+  } else {
+    struct Frags {
+      typename Num<T>::Frag p[FP], q[FQ];
+    };
+    int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
+    auto read = [&](Frags& f, const char* lp, const char* lq, int kk) __attribute__((always_inline)) {
+      // One register each: the fragments' addresses are made from it again
+      // every time (the registers are for the sums and two sets of fragments).
+      asm volatile("" : "+v"(rp_), "+v"(rq_));
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) f.q[j] = OQ::frag(lq, rq_, j, kk);
+#pragma unroll
+      for (int i = 0; i < FP; ++i) f.p[i] = OP::frag(lp, rp_, i, kk);
+    };
+    auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
+    };
+    // LDS reads, and a step's loads, one by one between the products.
+    auto interleave = [](auto loads_) __attribute__((always_inline)) {
+      constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ * (sizeof(T) == 4 ? 4 : 1);
+      constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
+      constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        if (i < reads) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+        }
+        if (i < loads) {
+          __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+        }
+      }
+      constexpr int rest = mmas - per * (reads + loads);
+      if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
+    };
+    // A step: the first half's fragments are in f0.  Reads its second half
+    // under the first half's products; then everyone's reads of this buffer are
+    // done and everyone's loads of the other have landed: the step after the
+    // next is sent for, and the next step's first half is read under the second
+    // half's products.
+    Frags f0, f1;
+    auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) __attribute__((always_inline)) {
+      read(f1, lp, lq, 1);
+      multiply(f0);
+      interleave(std::integral_constant<int, 0>());
+      __builtin_amdgcn_sched_barrier(0);
+      wait_and_meet<0>();
+      stage(s + 2, lp, lq);
+      read(f0, next_p, next_q, 0);
+      multiply(f1);
+      interleave(std::integral_constant<int, OP::kLoads + OQ::kLoads>());
+      __builtin_amdgcn_sched_barrier(0);
+    };
 
-  stage(0, p0, q0);
-  stage(1, p1, q1);
-  wait_and_meet<OP::kLoads + OQ::kLoads>();
-  read(f0, p0, q0, 0);
-  int s = 0;
-  for (; s + 2 <= nsteps; s += 2) {
-    body(s, p0, q0, p1, q1);
-    body(s + 1, p1, q1, p0, q0);
+    stage(0, p0, q0);
+    stage(1, p1, q1);
+    wait_and_meet<OP::kLoads + OQ::kLoads>();
+    read(f0, p0, q0, 0);
+    int s = 0;
+    for (; s + 2 <= nsteps; s += 2) {
+      body(s, p0, q0, p1, q1);
+      body(s + 1, p1, q1, p0, q0);
+    }
+    if (s < nsteps) body(s, p0, q0, p1, q1);
+    wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
   }
-  if (s < nsteps) body(s, p0, q0, p1, q1);
-  wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
 
   // ---- epilogue: acc[i][j] holds p = 16 i + 4 g + 0..3 of q = 16 j + lane % 16
   const int g = lane >> 4, c = lane & 15;
