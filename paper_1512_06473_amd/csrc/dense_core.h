@@ -131,8 +131,7 @@ __device__ __forceinline__ float act_slope(int act, float z) {
 
 enum EpiKind { kLinear = 0, kPartial = 1, kGated = 2, kStats = 3, kXgrad = 4 };
 
-// What becomes of a sum.  Quads are 4 consecutive p; with `vec` every array of
-// T here may be read and written 4 at a time where 4 are left.
+// What becomes of a sum.  Quads are 4 consecutive p.
 struct Epi {
   void* y;          // T [nq][ldy]: the result (kXgrad: the logits' gradient)
   void* pre;        // T [nq][ldpre] or null: the sum with its bias
@@ -143,7 +142,6 @@ struct Epi {
   long long ldy, ldpre, ldr, ldacc;
   int act;
   int acc_in, acc_out;  // add what is in acc; leave the sum there (no y)
-  int vec;
   // kStats, kXgrad: classes class0 .. class0 + np - 1 of `classes`
   const long long* labels;
   const float* lse;
@@ -155,34 +153,35 @@ struct Epi {
   int class0, classes;
 };
 
+// Four elements, or the n that are left.  Global memory takes them at any
+// address: rows of odd length need no other path.
 template <typename T>
-__device__ __forceinline__ f4 load_quad(const T* p, bool full, int n) {
-  typedef typename Num<T>::Quad Quad;
+__device__ __forceinline__ f4 load_quad(const T* p, int n) {
+  typename Num<T>::Quad t;
   f4 v = {0.f, 0.f, 0.f, 0.f};
-  if (full) {
-    const Quad t = *reinterpret_cast<const Quad*>(p);
+  if (n >= 4) {
+    __builtin_memcpy(&t, p, sizeof(t));
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < n) v[i] = (float)p[i];
   }
   return v;
 }
 
 template <typename T>
-__device__ __forceinline__ void store_quad(T* p, f4 v, bool full, int n) {
-  typedef typename Num<T>::Quad Quad;
-  if (full) {
-    Quad t;
+__device__ __forceinline__ void store_quad(T* p, f4 v, int n) {
+  typename Num<T>::Quad t;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
-    *reinterpret_cast<Quad*>(p) = t;
+  for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
+  if (n >= 4) {
+    __builtin_memcpy(p, &t, sizeof(t));
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) p[i] = (T)v[i];
+    for (int i = 0; i < 3; ++i)
+      if (i < n) p[i] = t[i];
   }
 }
 
@@ -190,21 +189,20 @@ template <typename T>
 __device__ __forceinline__ void emit_linear(const Epi& e, int np, int q, int p, f4 v) {
   const int n = np - p;
   if (n <= 0) return;
-  const bool full = e.vec && n >= 4;
   if (e.acc_in) v += *reinterpret_cast<const f4*>(e.acc + q * e.ldacc + p);
   if (e.acc_out) {
     *reinterpret_cast<f4*>(e.acc + q * e.ldacc + p) = v;
     return;
   }
   if (e.alpha) v *= *e.alpha;
-  if (e.bias) v += load_quad(static_cast<const T*>(e.bias) + p, full, n);
-  if (e.pre) store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, v, full, n);
+  if (e.bias) v += load_quad(static_cast<const T*>(e.bias) + p, n);
+  if (e.pre) store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, v, n);
   if (e.act != QCNN_ACT_NONE) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = act_value<T>(e.act, v[i]);
   }
-  if (e.res) v += load_quad(static_cast<const T*>(e.res) + q * e.ldr + p, full, n);
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, v, full, n);
+  if (e.res) v += load_quad(static_cast<const T*>(e.res) + q * e.ldr + p, n);
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, v, n);
 }
 
 // np: columns of the result (half of the weight's rows).
@@ -212,25 +210,24 @@ template <typename T>
 __device__ __forceinline__ void emit_gated(const Epi& e, int np, int q, int p, f4 g, f4 u) {
   const int n = np - p;
   if (n <= 0) return;
-  const bool full = e.vec && n >= 4;
   if (e.bias) {
-    g += load_quad(static_cast<const T*>(e.bias) + p, full, n);
-    u += load_quad(static_cast<const T*>(e.bias) + np + p, full, n);
+    g += load_quad(static_cast<const T*>(e.bias) + p, n);
+    u += load_quad(static_cast<const T*>(e.bias) + np + p, n);
   }
   if (e.pre) {
-    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, g, full, n);
-    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + np + p, u, full, n);
+    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, g, n);
+    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + np + p, u, n);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) g[i] = act_value<T>(e.act, g[i]) * u[i];
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, g, full, n);
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, g, n);
 }
 
 // Logits with their bias; classes past the end become -inf.
 template <typename T>
 __device__ __forceinline__ f4 class_logits(const Epi& e, int np, int p, f4 v) {
   const int n = np - p;
-  if (e.bias && n > 0) v += load_quad(static_cast<const T*>(e.bias) + e.class0 + p, e.vec && n >= 4, n);
+  if (e.bias && n > 0) v += load_quad(static_cast<const T*>(e.bias) + e.class0 + p, n);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i >= n) v[i] = -INFINITY;
@@ -258,7 +255,7 @@ __device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int q, int p, f
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (p + i >= np) d[i] = 0.f;
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, d, true, 4);
+  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, d, 4);
 }
 
 // (max, sum of exp(. - max)) of two disjoint sets.

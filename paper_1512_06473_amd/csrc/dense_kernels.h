@@ -32,99 +32,136 @@ bool wide(const void* p, long long ld, int cols) {  // rows of whole aligned 16 
   return ((uintptr_t)p & 15) == 0 && ld % u == 0 && cols % u == 0;
 }
 
-template <typename T>
-bool quads(const void* p, long long ld) {
-  return p == nullptr || (((uintptr_t)p & (4 * sizeof(T) - 1)) == 0 && ld % 4 == 0);
-}
-
 // ------------------------------------------------------ kernels around them
 
-// [rows][cols] with row stride ld -> rows of ldo, zeros past cols.
+// [rows][cols] with row stride ld -> rows of ldo, zeros past cols: a thread
+// writes 16 bytes.
 template <typename T>
 __global__ __launch_bounds__(256) void pad_kernel(const T* __restrict__ src, long long ld, int rows, int cols,
                                                   T* __restrict__ dst, int ldo) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= ldo) return;
-  for (int r = blockIdx.y; r < rows; r += gridDim.y) dst[(long long)r * ldo + c] = c < cols ? src[r * ld + c] : (T)0.f;
+  constexpr int kV = 16 / (int)sizeof(T);
+  const long long per = ldo / kV, all = rows * per;
+  for (long long id = blockIdx.x * 256LL + threadIdx.x; id < all; id += gridDim.x * 256LL) {
+    const long long r = id / per;
+    const int c = (int)(id % per) * kV;
+    const T* s = src + r * ld + c;
+    struct alignas(16) { T v[kV]; } t;
+    if (cols - c >= kV) {
+      __builtin_memcpy(&t, s, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kV; ++i) t.v[i] = c + i < cols ? s[i] : (T)0.f;
+    }
+    __builtin_memcpy(__builtin_assume_aligned(dst + r * ldo + c, 16), &t, 16);
+  }
 }
 
-// dz = dy act'(pre) (kGated: gate and up halves) and its sums over rows.
-// A thread has 4 columns and goes down `chunk` rows; the sums of a block's
-// rows go to part[blockIdx.y][columns of dz], joined by colsum_kernel: the
-// order of the additions is the same in every run.
+// dz = dy act'(pre) (gated: gate and up halves) and its sums over rows.  A
+// thread has 16 bytes of columns and goes down `chunk` rows, the loads of 4 at
+// a time; the sums of a block's rows go to part[blockIdx.y][columns of dz],
+// joined by colsum_kernel: the order of the additions is the same in every run.
 struct Slope {
   const void* dy;
   const void* pre;
   void* dz;     // null: only the sums
   float* part;  // null: no sums
   long long lddy, ldpre, lddz;
-  int rows, cols, chunk, act, vec;  // cols: of dy; vec: dy, pre, dz take quads
+  int rows, cols, chunk, act;  // cols: of dy
 };
 
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
-  const int p = (blockIdx.x * 256 + threadIdx.x) * 4;
-  const long long width = GATED ? 2 * a.cols : a.cols;
+  constexpr int kV = 16 / (int)sizeof(T), kQ = kV / 4;
+  const int p = (blockIdx.x * 256 + threadIdx.x) * kV;
+  const long long width = GATED ? 2LL * a.cols : a.cols;
+  const int r0 = blockIdx.y * a.chunk, r1 = min(a.rows, r0 + a.chunk);
   if (p >= a.cols) {
-    // the zeros between the columns and the row's end
-    if (a.dz && p < a.cols + 32) {
-      const long long col = width + (p - (a.cols + 3) / 4 * 4);
-      for (int r = blockIdx.y * a.chunk; r < min(a.rows, (blockIdx.y + 1) * a.chunk); ++r)
-        for (int i = 0; i < 4; ++i)
+    // the zeros between the columns and the row's end, fewer than kV
+    const long long col = width + (p - (a.cols + kV - 1) / kV * kV);
+    if (a.dz && p < a.cols + kV)
+      for (int r = r0; r < r1; ++r)
+        for (int i = 0; i < kV; ++i)
           if (col + i < a.lddz) static_cast<T*>(a.dz)[r * a.lddz + col + i] = (T)0.f;
-    }
     return;
   }
-  const int n = a.cols - p;
-  const bool full = a.vec && n >= 4;
-  f4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-  for (int r = blockIdx.y * a.chunk; r < min(a.rows, (blockIdx.y + 1) * a.chunk); ++r) {
-    const f4 dy = load_quad(static_cast<const T*>(a.dy) + r * a.lddy + p, full, n);
-    if constexpr (GATED) {
-      const T* z = static_cast<const T*>(a.pre) + r * a.ldpre + p;
-      const f4 g = load_quad(z, full, n), u = load_quad(z + a.cols, full, n);
-      f4 dg, du;
+  f4 s0[kQ], s1[kQ];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dg[i] = dy[i] * u[i] * act_slope<T>(a.act, g[i]);
-        du[i] = dy[i] * act_value<T>(a.act, g[i]);
-      }
-      T* o = static_cast<T*>(a.dz) + r * a.lddz + p;
-      store_quad(o, dg, full, n);
-      store_quad(o + a.cols, du, full, n);
-      s0 += dg;
-      s1 += du;
-    } else {
-      f4 d = dy;
-      if (a.act != QCNN_ACT_NONE) {
-        const f4 z = load_quad(static_cast<const T*>(a.pre) + r * a.ldpre + p, full, n);
+  for (int k = 0; k < kQ; ++k) s0[k] = s1[k] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int r = r0; r < r1; ++r) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] *= act_slope<T>(a.act, z[i]);
+    for (int k = 0; k < kQ; ++k) {
+      const int c = p + 4 * k, n = a.cols - c;
+      if (n <= 0) break;
+      const f4 dy = load_quad(static_cast<const T*>(a.dy) + r * a.lddy + c, n);
+      if constexpr (GATED) {
+        const T* z = static_cast<const T*>(a.pre) + r * a.ldpre + c;
+        const f4 g = load_quad(z, n), u = load_quad(z + a.cols, n);
+        f4 dg, du;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          dg[i] = dy[i] * u[i] * act_slope<T>(a.act, g[i]);
+          du[i] = dy[i] * act_value<T>(a.act, g[i]);
+        }
+        T* o = static_cast<T*>(a.dz) + r * a.lddz + c;
+        store_quad(o, dg, n);
+        store_quad(o + a.cols, du, n);
+        s0[k] += dg;
+        s1[k] += du;
+      } else {
+        f4 d = dy;
+        if (a.act != QCNN_ACT_NONE) {
+          const f4 z = load_quad(static_cast<const T*>(a.pre) + r * a.ldpre + c, n);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[i] *= act_slope<T>(a.act, z[i]);
+        }
+        if (a.dz) store_quad(static_cast<T*>(a.dz) + r * a.lddz + c, d, n);
+        s0[k] += d;
       }
-      if (a.dz) store_quad(static_cast<T*>(a.dz) + r * a.lddz + p, d, full, n);
-      s0 += d;
     }
   }
   if (a.part) {
     float* o = a.part + blockIdx.y * width + p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) {
-        o[i] = s0[i];
-        if (GATED) o[a.cols + i] = s1[i];
-      }
+    for (int k = 0; k < kQ; ++k) {
+      store_quad(o + 4 * k, s0[k], max(a.cols - p - 4 * k, 0));
+      if (GATED) store_quad(o + a.cols + 4 * k, s1[k], max(a.cols - p - 4 * k, 0));
+    }
   }
 }
 
-// out[c] = alpha sum_r part[r][c]
+// out[c] = alpha sum_r part[r][c]: 64 columns by 4 groups of rows.
 template <typename T>
 __global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ part, int rows, long long width,
                                                      const float* alpha, T* __restrict__ out) {
-  const long long c = blockIdx.x * 256LL + threadIdx.x;
-  if (c >= width) return;
+  __shared__ float group[4][64];
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
+  const long long c = blockIdx.x * 64LL + lane;
   float s = 0.f;
-  for (int r = 0; r < rows; ++r) s += part[r * width + c];
+  if (c < width) {
+#pragma unroll 8
+    for (int r = g; r < rows; r += 4) s += part[r * width + c];
+  }
+  group[g][lane] = s;
+  __syncthreads();
+  if (g != 0 || c >= width) return;
+  s = (s + group[1][lane]) + (group[2][lane] + group[3][lane]);
   out[c] = (T)(alpha ? s * *alpha : s);
+}
+
+// Rows of a thread: enough blocks for the chip, at most 512 rows of sums.
+inline int slope_chunk(int rows) { return std::max(16, ceil_div(rows, 512)); }
+
+// dz and, with dbias, alpha times its sums over rows.
+template <typename T, bool GATED>
+hipError_t run_slope(const Slope& a, void* dbias, const float* alpha, hipStream_t st) {
+  const int chunks = ceil_div(a.rows, a.chunk), width = GATED ? 2 * a.cols : a.cols;
+  const int threads = ceil_div(a.cols, 16 / (int)sizeof(T)) + 1;
+  slope_kernel<T, GATED><<<dim3(ceil_div(threads, 256), chunks), 256, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !dbias) return e;
+  colsum_kernel<T><<<ceil_div(width, 64), 256, 0, st>>>(a.part, chunks, width, alpha, static_cast<T*>(dbias));
+  return hipGetLastError();
 }
 
 // Sums of the parts of k, then the epilogue: a thread per quad of a row.
@@ -137,11 +174,13 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ p
   const long long each = (long long)nq * ldpart;
   const float* s = part + q * ldpart + p;
   f4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
-  if (p < np)
+  if (p < np) {
+#pragma unroll 8
     for (int i = 0; i < splits; ++i) {
       v += *reinterpret_cast<const f4*>(s + i * each);
       if (EPI == kGated) u += *reinterpret_cast<const f4*>(s + i * each + ldpart / 2);
     }
+  }
   if constexpr (EPI == kGated) emit_gated<T>(e, np, q, p, v, u);
   else if constexpr (EPI == kXgrad) emit_xgrad<T>(e, np, q, p, v);
   else emit_linear<T>(e, np, q, p, v);
@@ -155,9 +194,11 @@ __global__ __launch_bounds__(256) void finish_stats_kernel(const float* __restri
   const int q = (int)(id % nq), slot = (int)(id / nq), lane = threadIdx.x & 63, p = slot * 256 + lane * 4;
   if (slot >= slots) return;
   f4 z = {0.f, 0.f, 0.f, 0.f};
-  if (p < np)
+  if (p < np) {
+#pragma unroll 8
     for (int i = 0; i < splits; ++i)
       z += *reinterpret_cast<const f4*>(part + ((long long)i * nq + q) * ldpart + p);
+  }
   z = class_logits<T>(e, np, p, z);
   const long long label = e.labels[q] - e.class0;
   float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), sum = 0.f;
@@ -225,8 +266,7 @@ static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restri
 
 // ---------------------------------------------------------------- planning
 
-// A product's tiles and parts of k.  256 CUs: fewer tiles than that are split
-// along k, as long as a part keeps 4 steps to cover its first loads.
+// A product's tiles and parts of k.
 struct Cut {
   int big;  // 256 x 256 tiles of 8 waves, else 128 x 128 of 4
   int splits, steps;
@@ -238,24 +278,39 @@ inline long long tiles_of(int np, int nq, bool gated, int edge) {
   return (long long)ceil_div(np, gated ? edge / 2 : edge) * ceil_div(nq, edge);
 }
 
+// The cut that should take the least time: the steps in a row of the busiest
+// CU, times what one takes.  A CU holds one large tile or two small ones; two
+// small ones hide each other's waits.  Measured per step on whole products (k
+// of 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.68 to 0.83
+// us, two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32: 1.85,
+// 2.75, 4.2 to 4.7.  Parts of k are written and read once in fp32 (5 TB/s) and
+// take a second kernel.  Against the best of all measured cuts of ten shapes
+// the choice loses 0 to 12 %, against one fixed rule (256 workgroups) it gains
+// up to 1.4 times (1024 x 4096 -> 1024, fp32: 59 us, 71 with a part less per
+// CU).
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated) {
-  const long long small = tiles_of(np, nq, gated, 128), large = tiles_of(np, nq, gated, 256);
+  const double one = sizeof(T) == 4 ? 1.85 : 0.78, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
-  Cut c;
-  // Rounds of the chip times the work of a tile: a CU holds one large tile or
-  // two small ones at a time, and a large one moves half the LDS bytes per
-  // product.
-  const long long t_large = (large + 255) / 256 * 4 * 16, t_small = (small + 511) / 512 * 2 * 21;
-  c.big = t_large <= t_small;
-  const long long tiles = c.big ? large : small;
-  int splits = tiles >= 192 ? 1 : (int)std::min<long long>(256 / tiles, all / 4);
-  if (splits < 1) splits = 1;
-  c.steps = ceil_div(all, splits);
-  c.splits = ceil_div(all, c.steps);
-  c.ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
-  c.part_bytes = c.splits > 1 ? (size_t)c.splits * nq * c.ldpart * 4 : 0;
-  return c;
+  Cut best = {};
+  double least = 1e300;
+  for (int big = 0; big < 2; ++big) {
+    const long long tiles = tiles_of(np, nq, gated, big ? 256 : 128);
+    for (int n = 1; n <= 32 && (n == 1 || (n <= all / 2 && tiles * n <= 1024)); ++n) {
+      const int steps = ceil_div(all, n), splits = ceil_div(all, steps);
+      const long long groups = tiles * splits, rest = groups % 512;
+      const double rounds = big ? (groups + 255) / 256 * large : groups / 512 * two + (rest > 256 ? two : rest ? one : 0.);
+      const double t = steps * rounds + (splits > 1 ? 4. + 1.6e-6 * splits * nq * np * (gated ? 2 : 1) : 0.);
+      if (t >= least) continue;
+      least = t;
+      best.big = big;
+      best.splits = splits;
+      best.steps = steps;
+    }
+  }
+  best.ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
+  best.part_bytes = best.splits > 1 ? (size_t)best.splits * nq * best.ldpart * 4 : 0;
+  return best;
 }
 
 template <typename T, bool PS, bool QS, int EPI, bool GATED>
@@ -380,7 +435,8 @@ struct Source {
     if (!copy) return hipSuccess;
     T* o = reinterpret_cast<T*>(ws + at);
     const int ldo = pad16<T>(cols);
-    pad_kernel<T><<<dim3(ceil_div(ldo, 256), std::min(rows, 4096)), 256, 0, st>>>(p, ld, rows, cols, o, ldo);
+    const long long n = (long long)rows * (ldo / (16 / (int)sizeof(T)));
+    pad_kernel<T><<<(unsigned)std::min<long long>((n + 255) / 256, 1 << 20), 256, 0, st>>>(p, ld, rows, cols, o, ldo);
     p = o;
     ld = ldo;
     return hipGetLastError();
@@ -427,7 +483,6 @@ hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, co
   p.res = res;
   p.ldr = s.ldr;
   p.act = act;
-  p.vec = quads<T>(y, s.ldy) && quads<T>(pre, s.Ct) && quads<T>(bias, 4) && quads<T>(res, s.ldr);
   return c.template run<kLinear, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                       reinterpret_cast<float*>(ws.get() + part), st);
 }
@@ -453,12 +508,9 @@ hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, con
   p.ldpre = 2LL * s.Ct;
   p.bias = bias;
   p.act = act;
-  p.vec = s.Ct % 4 == 0 && quads<T>(y, s.ldy) && quads<T>(pre, 4) && quads<T>(bias, 4);
   return c.template run<kGated, true>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                     reinterpret_cast<float*>(ws.get() + part), st);
 }
-
-constexpr int kChunkRows = 64;  // rows whose bias gradients one thread adds up
 
 // dx = dz w, as fp32 running sums in `acc` or finished in y.
 template <typename T>
@@ -504,7 +556,7 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
   const bool in_place = !GATED && act == QCNN_ACT_NONE && (wide<T>(dy, s.ldy, s.Ct) || (!dx && !dw));
   const long long lddz = in_place ? s.ldy : pad16<T>(rows);
   const size_t dz_at = in_place ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
-  const int chunks = ceil_div(s.N, kChunkRows);
+  const int chunk = slope_chunk(s.N), chunks = ceil_div(s.N, chunk);
   const size_t sums_at = dbias ? l.add((size_t)chunks * rows * 4) : 0;
   Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
   const Cut cx = cut_of<T>(s.Cs, s.N, pad16<T>(rows), false), cw = cut_of<T>(s.Cs, rows, s.N, false);
@@ -528,16 +580,9 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     a.lddz = lddz;
     a.rows = s.N;
     a.cols = s.Ct;
-    a.chunk = kChunkRows;
+    a.chunk = chunk;
     a.act = act;
-    a.vec = quads<T>(dy, s.ldy) && quads<T>(pre, 4) && (!GATED ? quads<T>(pre, rows) : s.Ct % 4 == 0);
-    const int threads = ceil_div(s.Ct, 4) + (in_place ? 0 : 4);
-    slope_kernel<T, GATED><<<dim3(ceil_div(threads, 256), chunks), 256, 0, st>>>(a);
-    e = hipGetLastError();
-    if (e == hipSuccess && dbias) {
-      colsum_kernel<T><<<ceil_div(rows, 256), 256, 0, st>>>(a.part, chunks, rows, nullptr, static_cast<T*>(dbias));
-      e = hipGetLastError();
-    }
+    e = run_slope<T, GATED>(a, dbias, nullptr, st);
     if (e != hipSuccess) return e;
   }
   float* sums = reinterpret_cast<float*>(ws.get() + part);
@@ -545,7 +590,6 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Epi p = {};
     p.y = dx;
     p.ldy = s.Cs;
-    p.vec = quads<T>(dx, s.Cs);
     e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr(), rows, dz, lddz, s.N), p, cx, sums, st);
     if (e != hipSuccess) return e;
   }
@@ -553,7 +597,6 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Epi p = {};
     p.y = dw;
     p.ldy = s.Cs;
-    p.vec = quads<T>(dw, s.Cs);
     e = run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, rows), p, cw, sums, st);
   }
   return e;
@@ -576,7 +619,6 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   if (e != hipSuccess) return e;
   Epi p = {};
   p.bias = bias;
-  p.vec = quads<T>(bias, 4);
   p.labels = labels;
   p.stat = reinterpret_cast<float2*>(ws.get() + stat);
   p.zlabel = reinterpret_cast<float*>(ws.get() + zl);
@@ -609,7 +651,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   const long long ldd = pad16<T>(piece), ldacc = (s.Cs + 3) / 4 * 4;
   const size_t d_at = l.add((size_t)s.N * ldd * sizeof(T)), scale_at = l.add(8);
   const size_t acc_at = dx && pieces > 1 ? l.add((size_t)s.N * ldacc * 4) : 0;
-  const int chunks = ceil_div(s.N, kChunkRows);
+  const int chunk = slope_chunk(s.N), chunks = ceil_div(s.N, chunk);
   const size_t sums_at = dbias ? l.add((size_t)chunks * piece * 4) : 0;
   size_t part_bytes = 0;
   for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
@@ -638,7 +680,6 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
     p.y = d;
     p.ldy = ld;
     p.bias = bias;
-    p.vec = quads<T>(bias, 4) && c0 % 4 == 0;
     p.labels = labels;
     p.lse = lse;
     p.dloss = dloss;
@@ -655,18 +696,14 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       b.part = reinterpret_cast<float*>(ws.get() + sums_at);
       b.rows = s.N;
       b.cols = n;
-      b.chunk = kChunkRows;
+      b.chunk = chunk;
       b.act = QCNN_ACT_NONE;
-      b.vec = 1;
-      slope_kernel<T, false><<<dim3(ceil_div(ceil_div(n, 4), 256), chunks), 256, 0, st>>>(b);
-      colsum_kernel<T><<<ceil_div(n, 256), 256, 0, st>>>(b.part, chunks, n, scale + 1, static_cast<T*>(dbias) + c0);
-      e = hipGetLastError();
+      e = run_slope<T, false>(b, static_cast<T*>(dbias) + c0, scale + 1, st);
     }
     if (e == hipSuccess && dx) {
       Epi o = {};
       o.y = dx;
       o.ldy = s.Cs;
-      o.vec = quads<T>(dx, s.Cs);
       o.alpha = scale + 1;
       o.acc = reinterpret_cast<float*>(ws.get() + acc_at);
       o.ldacc = ldacc;
@@ -679,7 +716,6 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       Epi o = {};
       o.y = static_cast<T*>(dw) + (long long)c0 * s.Cs;
       o.ldy = s.Cs;
-      o.vec = quads<T>(o.y, s.Cs);
       o.alpha = scale + 1;
       e = run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, n), o, cut_of<T>(s.Cs, n, s.N, false), sums,
                                                      st);
