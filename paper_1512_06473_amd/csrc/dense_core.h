@@ -150,6 +150,7 @@ struct Epi {
   float gain;
   float2* stat;       // [slot][nq]: maximum and sum of exponentials of a slot's logits
   float* zlabel;      // [nq]: the label's logit
+  float *loss, *lse_out;  // [nq]: for the kernel that finishes a split product
   int class0, classes;
 };
 
@@ -407,13 +408,21 @@ __device__ __forceinline__ void tile_of(int id, int total, int tps, int tqs, int
 
 // WP x WQ outputs per wave.  kGated: the rows of a wave's P tile are WP / 2
 // gate rows and their up rows, so that a lane has both sums of a column.
-template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int EPI, bool GATED>
+template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int DEPTH, int EPI, bool GATED>
 __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(const Prod a, const Epi e) {
   constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
   static_assert(!GATED || !PS, "the gated layer's weights are read along k");
   typedef Operand<T, PS, BP, NW> OP;
   typedef Operand<T, QS, BQ, NW> OQ;
+  // One array per tile: the compiler then knows that a read of one does not
+  // wait for the loads into another.
+  static_assert(DEPTH == 2 || DEPTH == 4, "buffers");
   __shared__ __align__(16) char p0[OP::kBytes], p1[OP::kBytes], q0[OQ::kBytes], q1[OQ::kBytes];
+  __shared__ __align__(16) char p2[DEPTH > 2 ? OP::kBytes : 16], p3[DEPTH > 2 ? OP::kBytes : 16];
+  __shared__ __align__(16) char q2[DEPTH > 2 ? OQ::kBytes : 16], q3[DEPTH > 2 ? OQ::kBytes : 16];
+  char* const ps[4] = {p0, p1, p2, p3};
+  char* const qs[4] = {q0, q1, q2, q3};
+  constexpr int kFlight = OP::kLoads + OQ::kLoads;  // loads of a wave and step
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NWP, wq = wave / NWP;
@@ -504,15 +513,15 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
       }
     };
     auto loop = [&](auto split) __attribute__((always_inline)) {
-      stage(0, p0, q0);
-      for (int s = 0; s < nsteps; s += 2) {
-        wait_and_meet<0>();
-        stage(s + 1, p1, q1);
-        step(p0, q0, split);
-        if (s + 1 < nsteps) {
-          wait_and_meet<0>();
-          stage(s + 2, p0, q0);
-          step(p1, q1, split);
+#pragma unroll
+      for (int b = 0; b < DEPTH - 1; ++b) stage(b, ps[b], qs[b]);
+      for (int s = 0; s < nsteps; s += DEPTH) {
+#pragma unroll
+        for (int b = 0; b < DEPTH; ++b) {
+          if (s + b >= nsteps) break;
+          wait_and_meet<(DEPTH - 2) * kFlight>();
+          stage(s + b + DEPTH - 1, ps[(b + DEPTH - 1) % DEPTH], qs[(b + DEPTH - 1) % DEPTH]);
+          step(ps[b], qs[b], split);
         }
       }
       wait_and_meet<0>();
@@ -573,33 +582,35 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
     };
     // A step: the first half's fragments are in f0.  Reads its second half
     // under the first half's products; then everyone's reads of this buffer are
-    // done and everyone's loads of the other have landed: the step after the
-    // next is sent for, and the next step's first half is read under the second
-    // half's products.
+    // done and everyone's loads of the next have landed: the step that is DEPTH
+    // further on is sent for, and the next step's first half is read under the
+    // second half's products.
     Frags f0, f1;
     auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) __attribute__((always_inline)) {
       read(f1, lp, lq, 1);
       multiply(f0);
       interleave(std::integral_constant<int, 0>());
       __builtin_amdgcn_sched_barrier(0);
-      wait_and_meet<0>();
-      stage(s + 2, lp, lq);
+      wait_and_meet<(DEPTH - 2) * kFlight>();
+      stage(s + DEPTH, lp, lq);
       read(f0, next_p, next_q, 0);
       multiply(f1);
-      interleave(std::integral_constant<int, OP::kLoads + OQ::kLoads>());
+      interleave(std::integral_constant<int, kFlight>());
       __builtin_amdgcn_sched_barrier(0);
     };
 
-    stage(0, p0, q0);
-    stage(1, p1, q1);
-    wait_and_meet<OP::kLoads + OQ::kLoads>();
+#pragma unroll
+    for (int b = 0; b < DEPTH; ++b) stage(b, ps[b], qs[b]);
+    wait_and_meet<(DEPTH - 1) * kFlight>();
     read(f0, p0, q0, 0);
     int s = 0;
-    for (; s + 2 <= nsteps; s += 2) {
-      body(s, p0, q0, p1, q1);
-      body(s + 1, p1, q1, p0, q0);
+    for (; s + DEPTH <= nsteps; s += DEPTH) {
+#pragma unroll
+      for (int b = 0; b < DEPTH; ++b) body(s + b, ps[b], qs[b], ps[(b + 1) % DEPTH], qs[(b + 1) % DEPTH]);
     }
-    if (s < nsteps) body(s, p0, q0, p1, q1);
+#pragma unroll
+    for (int b = 0; b < DEPTH - 1; ++b)
+      if (s + b < nsteps) body(s + b, ps[b], qs[b], ps[b + 1], qs[b + 1]);
     wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
   }
 

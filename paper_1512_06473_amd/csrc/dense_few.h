@@ -1,4 +1,4 @@
-// Forward products of few rows: y[q][p] = sum_k w[p][k] x[q][k], q < 32.
+// Forward products of few rows: y[q][p] = sum_k w[p][k] x[q][k], q < 16 (fp32: 32).
 //
 // Every weight is used for a handful of products only, so the time is that of
 // reading w once, and what matters is how many bytes are on their way.  The

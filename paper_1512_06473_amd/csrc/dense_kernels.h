@@ -164,53 +164,88 @@ hipError_t run_slope(const Slope& a, void* dbias, const float* alpha, hipStream_
   return hipGetLastError();
 }
 
-// Sums of the parts of k, then the epilogue: a thread per quad of a row.
-template <typename T, int EPI>
+// Sums of the parts of k, then the epilogue: a thread per quad of a row, or,
+// with many parts (few outputs, that is), G threads that take every G-th part
+// (24 x 4096 -> 500 gated, 32 parts: 25 us with one, 13 with four).
+template <typename T, int EPI, int G>
 __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ part, int splits, long long ldpart,
                                                      int np, int nq, int quads_of_row, const Epi e) {
-  const long long id = blockIdx.x * 256LL + threadIdx.x;
+  constexpr int kQuads = 256 / G, kSums = EPI == kGated ? 2 : 1;
+  __shared__ f4 sums[G > 1 ? G - 1 : 1][kSums][kQuads];
+  const int t = threadIdx.x % kQuads, group = threadIdx.x / kQuads;
+  const long long id = blockIdx.x * (long long)kQuads + t;
   const int q = (int)(id / quads_of_row), p = (int)(id % quads_of_row) * 4;
-  if (q >= nq) return;
   const long long each = (long long)nq * ldpart;
   const float* s = part + q * ldpart + p;
   f4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
-  if (p < np) {
+  if (q < nq && p < np) {
 #pragma unroll 8
-    for (int i = 0; i < splits; ++i) {
+    for (int i = group; i < splits; i += G) {
       v += *reinterpret_cast<const f4*>(s + i * each);
       if (EPI == kGated) u += *reinterpret_cast<const f4*>(s + i * each + ldpart / 2);
     }
   }
+  if constexpr (G > 1) {
+    if (group > 0) {
+      sums[group - 1][0][t] = v;
+      if (EPI == kGated) sums[group - 1][kSums - 1][t] = u;
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 0; i < G - 1; ++i) {
+      v += sums[i][0][t];
+      if (EPI == kGated) u += sums[i][kSums - 1][t];
+    }
+  }
+  if (q >= nq) return;
   if constexpr (EPI == kGated) emit_gated<T>(e, np, q, p, v, u);
   else if constexpr (EPI == kXgrad) emit_xgrad<T>(e, np, q, p, v);
   else emit_linear<T>(e, np, q, p, v);
 }
 
-// The same for the loss: a wave per row and 256 classes.
+__device__ __forceinline__ void write_loss(float2 t, float zlabel, long long label, int classes, float* loss,
+                                           float* lse) {
+  const float l = t.x + logf(t.y);
+  *lse = l;
+  *loss = label < 0 ? 0.f : label >= classes ? NAN : l - zlabel;
+}
+
+// The same for the loss: a workgroup per row and `width` classes, which
+// finishes the row where that is all of them, else leaves a slot's statistics.
 template <typename T>
-__global__ __launch_bounds__(256) void finish_stats_kernel(const float* __restrict__ part, int splits,
-                                                           long long ldpart, int np, int nq, int slots, const Epi e) {
-  const long long id = blockIdx.x * 4LL + (threadIdx.x >> 6);
-  const int q = (int)(id % nq), slot = (int)(id / nq), lane = threadIdx.x & 63, p = slot * 256 + lane * 4;
-  if (slot >= slots) return;
-  f4 z = {0.f, 0.f, 0.f, 0.f};
-  if (p < np) {
+__global__ __launch_bounds__(256) void finish_loss_kernel(const float* __restrict__ part, int splits,
+                                                          long long ldpart, int np, int nq, int width, const Epi e) {
+  __shared__ float2 stats[4];
+  __shared__ float zlabel;
+  const int q = blockIdx.x, end = min(np, (int)(blockIdx.y + 1) * width);
+  const long long label = e.labels[q], each = (long long)nq * ldpart;
+  float2 t = make_float2(-INFINITY, 0.f);
+  for (int p = blockIdx.y * width + threadIdx.x * 4; p < end; p += 1024) {
+    f4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int i = 0; i < splits; ++i)
-      z += *reinterpret_cast<const f4*>(part + ((long long)i * nq + q) * ldpart + p);
-  }
-  z = class_logits<T>(e, np, p, z);
-  const long long label = e.labels[q] - e.class0;
-  float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), sum = 0.f;
+    for (int i = 0; i < splits; ++i) z += *reinterpret_cast<const f4*>(part + i * each + q * ldpart + p);
+    z = class_logits<T>(e, np, p, z);
+    const float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+    float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (label == p + i && p + i < np) e.zlabel[q] = z[i];
-    sum += z[i] == -INFINITY ? 0.f : __expf(z[i] - m);
+    for (int i = 0; i < 4; ++i) {
+      if (label == p + i && p + i < np) {
+        zlabel = z[i];
+        if (e.stat) e.zlabel[q] = z[i];
+      }
+      sum += z[i] == -INFINITY ? 0.f : __expf(z[i] - m);
+    }
+    t = join_stat(t, make_float2(m, sum));
   }
-  float2 t = make_float2(m, sum);
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));
-  if (lane == 0) e.stat[(long long)slot * nq + q] = t;
+  if ((threadIdx.x & 63) == 0) stats[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x) return;
+  t = join_stat(join_stat(stats[0], stats[1]), join_stat(stats[2], stats[3]));
+  if (e.stat) e.stat[(long long)blockIdx.y * nq + q] = t;
+  else write_loss(t, zlabel, label, e.classes, e.loss + q, e.lse_out + q);
 }
 
 // Joins the slots' maxima and sums of each row: ROWS rows by 256 / ROWS
@@ -235,11 +270,7 @@ static __global__ __launch_bounds__(256) void loss_kernel(const float2* __restri
     if (r < n) part[r][c] = join_stat(part[r][c], part[r + n][c]);
   }
   if (r != 0 || q >= nq) return;
-  t = part[0][c];
-  const float l = t.x + logf(t.y);
-  const long long label = labels[q];
-  lse[q] = l;
-  loss[q] = label < 0 ? 0.f : label >= classes ? NAN : l - zlabel[q];
+  write_loss(part[0][c], zlabel[q], labels[q], classes, loss + q, lse + q);
 }
 
 // out[0] = the largest finite |dloss| of a counted row (1 if there is none or
@@ -281,16 +312,16 @@ inline long long tiles_of(int np, int nq, bool gated, int edge) {
 // The cut that should take the least time: the steps in a row of the busiest
 // CU, times what one takes.  A CU holds one large tile or two small ones; two
 // small ones hide each other's waits.  Measured per step on whole products (k
-// of 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.68 to 0.83
-// us, two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32: 1.85,
+// of 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.6 to 0.75
+// us, two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32: 1.6,
 // 2.75, 4.2 to 4.7.  Parts of k are written and read once in fp32 (5 TB/s) and
 // take a second kernel.  Against the best of all measured cuts of ten shapes
 // the choice loses 0 to 12 %, against one fixed rule (256 workgroups) it gains
-// up to 1.4 times (1024 x 4096 -> 1024, fp32: 59 us, 71 with a part less per
+// up to 1.4 times (1024 x 4096 -> 1024 in fp32: 57 us, 64 with one workgroup per
 // CU).
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated) {
-  const double one = sizeof(T) == 4 ? 1.85 : 0.78, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
+  const double one = sizeof(T) == 4 ? 1.6 : 0.66, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
   Cut best = {};
   double least = 1e300;
@@ -318,21 +349,30 @@ hipError_t launch_product(const Prod& a, const Epi& e, const Cut& c, hipStream_t
   LaunchTimer timer;
   const dim3 grid((unsigned)tiles_of(a.np, a.nq, GATED, c.big ? 256 : 128) * c.splits);
   if (c.big)
-    return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
-  return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+    return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, 2, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
+  if (grid.x <= 256)  // one workgroup per CU: its LDS holds four steps (1024 x 4096 -> 1024 bf16: 45 us, with four 39)
+    return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 4, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+  return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 2, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
 }
+
+// Classes of a workgroup of finish_loss_kernel; slots of statistics that it
+// leaves (none if it finishes the rows).
+inline int loss_width(int np) { return np <= 4096 ? 4096 : 1024; }
+inline int loss_slots(int np) { return np <= 4096 ? 0 : ceil_div(np, 1024); }
 
 // After kPartial: the parts' sums and the epilogue.
 template <typename T, int EPI>
 hipError_t finish(int np, int nq, const Epi& e, const Cut& c, const float* part, hipStream_t st) {
   if constexpr (EPI == kStats) {
-    const int slots = ceil_div(np, 256);
-    const long long waves = (long long)slots * nq;
-    finish_stats_kernel<T><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, slots, e);
+    const int width = loss_width(np);
+    finish_loss_kernel<T><<<dim3(nq, ceil_div(np, width)), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, width, e);
   } else {
     const int per = EPI == kXgrad ? (int)(e.ldy / 4) : ceil_div(np, 4);
     const long long n = (long long)per * nq;
-    finish_kernel<T, EPI><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, per, e);
+    if (c.splits >= 8)
+      finish_kernel<T, EPI, 4><<<(unsigned)((n + 63) / 64), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, per, e);
+    else
+      finish_kernel<T, EPI, 1><<<(unsigned)((n + 255) / 256), 256, 0, st>>>(part, c.splits, c.ldpart, np, nq, per, e);
   }
   return hipGetLastError();
 }
@@ -348,22 +388,24 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   return err != hipSuccess ? err : finish<T, EPI>(a.np, a.nq, e, c, part, st);
 }
 
-// A forward product: the tiles, or for at most 32 rows the kernel that
-// streams the weights.
-constexpr int kFewRows = 32;
+// A forward product: the tiles, or for few rows the kernel that streams the
+// weights.  At 24 rows (4096 -> 4096, 9216 -> 4096, 4096 -> 22016) it takes 16,
+// 29 and 58 us in bf16, the tiles 15, 23 and 49; in fp32 27, 50 and 109 against
+// 34, 62 and 160 (at 33 rows 35, 68 and 152 against 34, 61 and 158).
+template <typename T>
+constexpr int kFewRows = sizeof(T) == 4 ? 32 : 16;
 
 template <typename T>
 struct Forward : Cut {
   bool few, wide_ = false;
-  int ks, slots;  // slots: of kStats
+  int ks, slots;  // slots: of kStats, 0 where the parts' sums go straight to the loss
   int np, nq, nk;
   bool gated;
   Forward(int np_, int nq_, int nk_, bool gated_) : np(np_), nq(nq_), nk(nk_), gated(gated_) {
-    few = nq <= kFewRows;
+    few = nq <= kFewRows<T>;
     if (!few) {
       static_cast<Cut&>(*this) = cut_of<T>(np, nq, pad16<T>(nk), gated);
-      // one per wave along p (2 in a tile), or per 256 classes after a split
-      slots = splits > 1 ? ceil_div(np, 256) : 2 * ceil_div(np, big ? 256 : 128);
+      slots = splits > 1 ? loss_slots(np) : 2 * ceil_div(np, big ? 256 : 128);  // one per wave along p, 2 in a tile
       return;
     }
     // A wave's 16 rows (32 past 8 rows of x and where there are many, whose
@@ -382,7 +424,7 @@ struct Forward : Cut {
     splits = ceil_div(all, ks * steps);
     ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
     part_bytes = splits > 1 ? (size_t)splits * nq * ldpart * 4 : 0;
-    slots = splits > 1 ? ceil_div(np, 256) : ceil_div(np, cols());
+    slots = splits > 1 ? loss_slots(np) : ceil_div(np, cols());
   }
 
   int cols() const { return wide_ ? 32 : 16; }  // result columns of a wave
@@ -391,7 +433,8 @@ struct Forward : Cut {
   hipError_t launch_few(const Few& a, const Epi& e, hipStream_t st) const {
     LaunchTimer timer;
     const dim3 grid((unsigned)(ceil_div(ceil_div(np, cols()), kFewWaves / ks) * splits)), block(64 * kFewWaves);
-    if (nq > 16) return timed_launch(&timer, few_kernel<T, 2, 2, EPI, GATED>, grid, block, 0u, st, a, e);
+    if constexpr (kFewRows<T> > 16)
+      if (nq > 16) return timed_launch(&timer, few_kernel<T, 2, 2, EPI, GATED>, grid, block, 0u, st, a, e);
     if constexpr (!GATED)
       if (!wide_) return timed_launch(&timer, few_kernel<T, 1, 1, EPI, GATED>, grid, block, 0u, st, a, e);
     return timed_launch(&timer, few_kernel<T, 2, 1, EPI, GATED>, grid, block, 0u, st, a, e);
@@ -620,12 +663,14 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   Epi p = {};
   p.bias = bias;
   p.labels = labels;
-  p.stat = reinterpret_cast<float2*>(ws.get() + stat);
+  p.stat = slots ? reinterpret_cast<float2*>(ws.get() + stat) : nullptr;
   p.zlabel = reinterpret_cast<float*>(ws.get() + zl);
   p.classes = s.Ct;
+  p.loss = loss;
+  p.lse_out = lse;
   e = c.template run<kStats, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
                                                   reinterpret_cast<float*>(ws.get() + part), st);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || slots == 0) return e;
   // 16 rows read whole 128-byte lines; fewer than 64 rows would leave most of
   // the chip idle and go down hundreds of slots one after another.
   if (s.N >= 64)
@@ -643,7 +688,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
                          const float* lse, const float* dloss, void* dx, void* dw, void* dbias, const Room& room,
                          hipStream_t st) {
   Layout l;
-  const bool few = s.N <= kFewRows;
+  const bool few = s.N <= kFewRows<T>;
   Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !few || dw), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !few || dx);
   long long fit = (long long)(kPieceBytes / ((size_t)s.N * sizeof(T))) / 256 * 256;
   if (fit < 256) fit = 256;
