@@ -60,6 +60,8 @@ struct Num<float> {
   }
   static __device__ __forceinline__ float exp_(float x) { return expf(x); }
   static __device__ __forceinline__ float div_(float a, float b) { return a / b; }
+  // The normal distribution function; density = exp(-z^2 / 2).
+  static __device__ __forceinline__ float phi(float z, float) { return 0.5f * (1.f + erff(z * 0.70710678118654752f)); }
 };
 
 // 16-bit results carry 8 or 11 bits: the hardware's exponential and reciprocal
@@ -67,6 +69,15 @@ struct Num<float> {
 struct Num16 {
   static __device__ __forceinline__ float exp_(float x) { return __expf(x); }
   static __device__ __forceinline__ float div_(float a, float b) { return a * __builtin_amdgcn_rcpf(b); }
+  // Phi(-|z|) = exp(-z^2 / 2) t Q(t), t = 1 / (1 + c |z|), with Q the polynomial
+  // of degree 6 that fits Phi(-|z|) exp(z^2 / 2) / t over |z| < 28 best in the
+  // largest relative error, 2e-6: a sixth of erff's instructions, and the
+  // slope's exponential with it (4096 x 4096 slopes: 45 us with erff).
+  static __device__ __forceinline__ float phi(float z, float density) {
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.371231049f * fabsf(z));
+    const float tail = density * t * (0.148124367f + t * (0.14742066f + t * (0.134845033f + t * (0.0494158827f + t * (0.139162809f + t * (-0.166493893f + t * (0.0475246012f)))))));
+    return z > 0.f ? 1.f - tail : tail;
+  }
 };
 
 template <>
@@ -99,7 +110,7 @@ template <typename T>
 __device__ __forceinline__ float act_value(int act, float z) {
   switch (act) {
     case QCNN_ACT_RELU: return z > 0.f ? z : z != z ? z : 0.f;
-    case QCNN_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case QCNN_ACT_GELU: return z * Num<T>::phi(z, Num<T>::exp_(-0.5f * z * z));
     case QCNN_ACT_GELU_TANH: {  // 1 + tanh(u) = 2 / (1 + exp(-2 u))
       const float u2 = 1.5957691216057308f * (z + 0.044715f * z * z * z);
       return Num<T>::div_(z, 1.f + Num<T>::exp_(-u2));
@@ -113,8 +124,10 @@ template <typename T>
 __device__ __forceinline__ float act_slope(int act, float z) {
   switch (act) {
     case QCNN_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case QCNN_ACT_GELU:
-      return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + 0.39894228040143268f * z * Num<T>::exp_(-0.5f * z * z);
+    case QCNN_ACT_GELU: {
+      const float density = Num<T>::exp_(-0.5f * z * z);
+      return Num<T>::phi(z, density) + 0.39894228040143268f * z * density;
+    }
     case QCNN_ACT_GELU_TANH: {
       const float s = Num<T>::div_(1.f, 1.f + Num<T>::exp_(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
       return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);

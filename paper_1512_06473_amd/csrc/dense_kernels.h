@@ -69,6 +69,33 @@ struct Slope {
   int rows, cols, chunk, act;  // cols: of dy
 };
 
+// 16 bytes of elements, or the n that are left.
+template <typename T, int Q>
+__device__ __forceinline__ void load_wide(const T* p, int n, f4 (&v)[Q]) {
+  if (n >= 4 * Q) {
+    typename Num<T>::Frag t;
+    __builtin_memcpy(&t, p, 16);
+#pragma unroll
+    for (int i = 0; i < 4 * Q; ++i) v[i / 4][i % 4] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int k = 0; k < Q; ++k) v[k] = load_quad(p + 4 * k, n - 4 * k);
+  }
+}
+
+template <typename T, int Q>
+__device__ __forceinline__ void store_wide(T* p, int n, const f4 (&v)[Q]) {
+  if (n >= 4 * Q) {
+    typename Num<T>::Frag t;
+#pragma unroll
+    for (int i = 0; i < 4 * Q; ++i) t[i] = (T)v[i / 4][i % 4];
+    __builtin_memcpy(p, &t, 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < Q; ++k) store_quad(p + 4 * k, v[k], n - 4 * k);
+  }
+}
+
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
   constexpr int kV = 16 / (int)sizeof(T), kQ = kV / 4;
@@ -87,45 +114,48 @@ __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
   f4 s0[kQ], s1[kQ];
 #pragma unroll
   for (int k = 0; k < kQ; ++k) s0[k] = s1[k] = f4{0.f, 0.f, 0.f, 0.f};
+  const int n = a.cols - p;
 #pragma unroll 4
   for (int r = r0; r < r1; ++r) {
+    f4 dy[kQ], g[kQ], u[kQ];
+    load_wide(static_cast<const T*>(a.dy) + r * a.lddy + p, n, dy);
+    if constexpr (GATED) {
+      const T* z = static_cast<const T*>(a.pre) + r * a.ldpre + p;
+      load_wide(z, n, g);
+      load_wide(z + a.cols, n, u);
 #pragma unroll
-    for (int k = 0; k < kQ; ++k) {
-      const int c = p + 4 * k, n = a.cols - c;
-      if (n <= 0) break;
-      const f4 dy = load_quad(static_cast<const T*>(a.dy) + r * a.lddy + c, n);
-      if constexpr (GATED) {
-        const T* z = static_cast<const T*>(a.pre) + r * a.ldpre + c;
-        const f4 g = load_quad(z, n), u = load_quad(z + a.cols, n);
-        f4 dg, du;
+      for (int k = 0; k < kQ; ++k) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          dg[i] = dy[i] * u[i] * act_slope<T>(a.act, g[i]);
-          du[i] = dy[i] * act_value<T>(a.act, g[i]);
+          const float d = dy[k][i], z = g[k][i];
+          g[k][i] = d * u[k][i] * act_slope<T>(a.act, z);
+          u[k][i] = d * act_value<T>(a.act, z);
         }
-        T* o = static_cast<T*>(a.dz) + r * a.lddz + c;
-        store_quad(o, dg, n);
-        store_quad(o + a.cols, du, n);
-        s0[k] += dg;
-        s1[k] += du;
-      } else {
-        f4 d = dy;
-        if (a.act != QCNN_ACT_NONE) {
-          const f4 z = load_quad(static_cast<const T*>(a.pre) + r * a.ldpre + c, n);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) d[i] *= act_slope<T>(a.act, z[i]);
-        }
-        if (a.dz) store_quad(static_cast<T*>(a.dz) + r * a.lddz + c, d, n);
-        s0[k] += d;
+        s0[k] += g[k];
+        s1[k] += u[k];
       }
+      T* o = static_cast<T*>(a.dz) + r * a.lddz + p;
+      store_wide(o, n, g);
+      store_wide(o + a.cols, n, u);
+    } else {
+      if (a.act != QCNN_ACT_NONE) {
+        load_wide(static_cast<const T*>(a.pre) + r * a.ldpre + p, n, g);
+#pragma unroll
+        for (int k = 0; k < kQ; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) dy[k][i] *= act_slope<T>(a.act, g[k][i]);
+      }
+      if (a.dz) store_wide(static_cast<T*>(a.dz) + r * a.lddz + p, n, dy);
+#pragma unroll
+      for (int k = 0; k < kQ; ++k) s0[k] += dy[k];
     }
   }
   if (a.part) {
     float* o = a.part + blockIdx.y * width + p;
 #pragma unroll
     for (int k = 0; k < kQ; ++k) {
-      store_quad(o + 4 * k, s0[k], max(a.cols - p - 4 * k, 0));
-      if (GATED) store_quad(o + a.cols + 4 * k, s1[k], max(a.cols - p - 4 * k, 0));
+      store_quad(o + 4 * k, s0[k], n - 4 * k);
+      if (GATED) store_quad(o + a.cols + 4 * k, s1[k], n - 4 * k);
     }
   }
 }
@@ -150,7 +180,7 @@ __global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ p
 }
 
 // Rows of a thread: enough blocks for the chip, at most 512 rows of sums.
-inline int slope_chunk(int rows) { return std::max(16, ceil_div(rows, 512)); }
+inline int slope_chunk(int rows) { return std::max(4, ceil_div(rows, 512)); }
 
 // dz and, with dbias, alpha times its sums over rows.
 template <typename T, bool GATED>
@@ -321,7 +351,7 @@ inline long long tiles_of(int np, int nq, bool gated, int edge) {
 // CU).
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated) {
-  const double one = sizeof(T) == 4 ? 1.6 : 0.66, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
+  const double one = sizeof(T) == 4 ? 1.85 : 0.66, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
   Cut best = {};
   double least = 1e300;
