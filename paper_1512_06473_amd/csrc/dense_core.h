@@ -291,6 +291,8 @@ struct Prod {
   int kp, kq;           // rows that an S operand has (C: unused)
   int colsp, colsq;     // columns that an S operand stores, whole 16 bytes
   int p2;               // kGated: rows between a gate row and its up row
+  int p0, p1, q0, q1;   // the outputs of this launch; kStats: their first slot
+  int slot0;
   int splits, steps;    // parts of k; steps of 128 bytes in each
   float* part;          // kPartial: fp32 [splits][nq][ldpart]
   long long ldpart;     // kGated's sums: gate at p, up at ldpart / 2 + p
@@ -440,10 +442,10 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NWP, wq = wave / NWP;
   constexpr int BC = GATED ? BP / 2 : BP;  // result columns of a tile
-  const int tps = (a.np + BC - 1) / BC, tqs = (a.nq + BQ - 1) / BQ;
+  const int tps = (a.p1 - a.p0 + BC - 1) / BC, tqs = (a.q1 - a.q0 + BQ - 1) / BQ;
   int tp, tq, split;
   tile_of(blockIdx.x, gridDim.x, tps, tqs, &tp, &tq, &split);
-  const int cp = tp * BC, cq = tq * BQ;
+  const int cp = a.p0 + tp * BC, cq = a.q0 + tq * BQ;
   const int step0 = split * a.steps;
   const int all = (a.nk * (int)sizeof(T) + 127) / 128;
   const int nsteps = min(a.steps, all - step0);
@@ -656,7 +658,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
       float2 t = make_float2(m, sum);
 #pragma unroll
       for (int o = 16; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));
-      if (g == 0 && q < a.nq) e.stat[(long long)(tp * NWP + wp) * a.nq + q] = t;
+      if (g == 0 && q < a.nq) e.stat[(long long)(a.slot0 + tp * NWP + wp) * a.nq + q] = t;
     }
   } else {
     // Through LDS, a wave's 16 KB of it: 64 lanes in the products' order hold

@@ -330,6 +330,7 @@ static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restri
 // A product's tiles and parts of k.
 struct Cut {
   int big;  // 256 x 256 tiles of 8 waves, else 128 x 128 of 4
+  int main_p, main_q;  // large tiles along one axis (0: all), the rest in small ones
   int splits, steps;
   size_t part_bytes;
   long long ldpart;
@@ -349,18 +350,24 @@ inline long long tiles_of(int np, int nq, bool gated, int edge) {
 // the choice loses 0 to 12 %, against one fixed rule (256 workgroups) it gains
 // up to 1.4 times (1024 x 4096 -> 1024 in fp32: 57 us, 64 with one workgroup per
 // CU).
+// A last round of large tiles that would leave most CUs idle goes in small ones
+// (1999 rows to 50001 classes: 6.1 rounds).  rows_alike: not along q.
 template <typename T>
-Cut cut_of(int np, int nq, int nk, bool gated) {
+Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
   const double one = sizeof(T) == 4 ? 1.85 : 0.66, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
+  auto small_rounds = [&](long long groups) {
+    const long long rest = groups % 512;
+    return groups / 512 * two + (rest > 256 ? two : rest ? one : 0.);
+  };
   Cut best = {};
   double least = 1e300;
   for (int big = 0; big < 2; ++big) {
     const long long tiles = tiles_of(np, nq, gated, big ? 256 : 128);
     for (int n = 1; n <= 32 && (n == 1 || (n <= all / 2 && tiles * n <= 1024)); ++n) {
       const int steps = ceil_div(all, n), splits = ceil_div(all, steps);
-      const long long groups = tiles * splits, rest = groups % 512;
-      const double rounds = big ? (groups + 255) / 256 * large : groups / 512 * two + (rest > 256 ? two : rest ? one : 0.);
+      const long long groups = tiles * splits;
+      const double rounds = big ? (groups + 255) / 256 * large : small_rounds(groups);
       const double t = steps * rounds + (splits > 1 ? 4. + 1.6e-6 * splits * nq * np * (gated ? 2 : 1) : 0.);
       if (t >= least) continue;
       least = t;
@@ -369,20 +376,50 @@ Cut cut_of(int np, int nq, int nk, bool gated) {
       best.steps = steps;
     }
   }
+  const int width = gated ? 128 : 256, tps = ceil_div(np, width), tqs = ceil_div(nq, 256);
+  const long long rounds = (long long)tps * tqs / 256;
+  for (int axis = 0; axis < (rows_alike ? 1 : 2) && rounds > 0; ++axis) {
+    const int mine = axis ? tqs : tps, other = axis ? tps : tqs;
+    const int main = (int)(rounds * 256 / other);
+    if (main < 1 || main >= mine) continue;
+    const long long tail = axis ? tiles_of(np, nq - main * 256, gated, 128) : tiles_of(np - main * width, nq, gated, 128);
+    const double t = all * (((long long)main * other + 255) / 256 * large + small_rounds(tail)) + 4.;
+    if (t >= least) continue;
+    least = t;
+    best.big = best.splits = 1;
+    best.steps = all;
+    best.main_p = axis ? 0 : main;
+    best.main_q = axis ? main : 0;
+  }
   best.ldpart = (long long)ceil_div(np, 4) * 4 * (gated ? 2 : 1);
   best.part_bytes = best.splits > 1 ? (size_t)best.splits * nq * best.ldpart * 4 : 0;
   return best;
 }
 
+// The tiles of outputs [p0, p1) x [q0, q1).
 template <typename T, bool PS, bool QS, int EPI, bool GATED>
-hipError_t launch_product(const Prod& a, const Epi& e, const Cut& c, hipStream_t st) {
+hipError_t launch_tiles(Prod a, const Epi& e, bool big, int p0, int p1, int q0, int q1, hipStream_t st) {
+  a.p0 = p0;
+  a.p1 = p1;
+  a.q0 = q0;
+  a.q1 = q1;
   LaunchTimer timer;
-  const dim3 grid((unsigned)tiles_of(a.np, a.nq, GATED, c.big ? 256 : 128) * c.splits);
-  if (c.big)
+  const dim3 grid((unsigned)tiles_of(p1 - p0, q1 - q0, GATED, big ? 256 : 128) * a.splits);
+  if (big)
     return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, 2, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
   if (grid.x <= 256)  // one workgroup per CU: its LDS holds four steps (1024 x 4096 -> 1024 bf16: 45 us, with four 39)
     return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 4, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
   return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 2, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+}
+
+template <typename T, bool PS, bool QS, int EPI, bool GATED>
+hipError_t launch_product(Prod a, const Epi& e, const Cut& c, hipStream_t st) {
+  const int p = c.main_p * (GATED ? 128 : 256), q = c.main_q * 256;
+  if (!p && !q) return launch_tiles<T, PS, QS, EPI, GATED>(a, e, c.big, 0, a.np, 0, a.nq, st);
+  const hipError_t err = launch_tiles<T, PS, QS, EPI, GATED>(a, e, true, 0, p ? p : a.np, 0, q ? q : a.nq, st);
+  if (err != hipSuccess) return err;
+  if (p) a.slot0 = 2 * c.main_p;
+  return launch_tiles<T, PS, QS, EPI, GATED>(a, e, false, p, a.np, q, a.nq, st);
 }
 
 // Classes of a workgroup of finish_loss_kernel; slots of statistics that it
@@ -418,6 +455,13 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   return err != hipSuccess ? err : finish<T, EPI>(a.np, a.nq, e, c, part, st);
 }
 
+// Slots of a product that is not split: one per wave along p, 2 in a tile (the
+// same for every row, so none of its rows may go in tiles of another size).
+inline int stat_slots(const Cut& c, int np) {
+  if (c.main_p) return 2 * c.main_p + 2 * ceil_div(np - c.main_p * 256, 128);
+  return 2 * ceil_div(np, c.big ? 256 : 128);
+}
+
 // A forward product: the tiles, or for few rows the kernel that streams the
 // weights.  At 24 rows (4096 -> 4096, 9216 -> 4096, 4096 -> 22016) it takes 16,
 // 29 and 58 us in bf16, the tiles 15, 23 and 49; in fp32 27, 50 and 109 against
@@ -431,11 +475,12 @@ struct Forward : Cut {
   int ks, slots;  // slots: of kStats, 0 where the parts' sums go straight to the loss
   int np, nq, nk;
   bool gated;
-  Forward(int np_, int nq_, int nk_, bool gated_) : np(np_), nq(nq_), nk(nk_), gated(gated_) {
+  Forward(int np_, int nq_, int nk_, bool gated_, bool rows_alike = false)
+      : np(np_), nq(nq_), nk(nk_), gated(gated_) {
     few = nq <= kFewRows<T>;
     if (!few) {
-      static_cast<Cut&>(*this) = cut_of<T>(np, nq, pad16<T>(nk), gated);
-      slots = splits > 1 ? loss_slots(np) : 2 * ceil_div(np, big ? 256 : 128);  // one per wave along p, 2 in a tile
+      static_cast<Cut&>(*this) = cut_of<T>(np, nq, pad16<T>(nk), gated, rows_alike);
+      slots = splits > 1 ? loss_slots(np) : stat_slots(*this, np);
       return;
     }
     // A wave's 16 rows (32 past 8 rows of x and where there are many, whose
@@ -679,7 +724,7 @@ template <typename T>
 hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, const void* bias, const long long* labels,
                         float* loss, float* lse, const Room& room, hipStream_t st) {
   Layout l;
-  const Forward<T> c(s.Ct, s.N, s.Cs, false);
+  const Forward<T> c(s.Ct, s.N, s.Cs, false, true);
   Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few);
   const int slots = c.slots;
   const size_t part = l.add(c.part_bytes), stat = l.add((size_t)slots * s.N * 8), zl = l.add((size_t)s.N * 4);
