@@ -362,25 +362,20 @@ struct Operand {
   }
 };
 
-// Eight fp32 values as three bf16 parts each: the upper 8 bits of the 24, the
+// Four fp32 values as three bf16 parts each: the upper 8 bits of the 24, the
 // next 8, the last 8, each cut off (not rounded, so that nothing overflows),
 // which is exact.  Of the nine products of two numbers' parts the three
 // smallest, below 2^-22 of the whole, are left out.
-__device__ __forceinline__ void split_bf16(f4 a, f4 b, b8 (&out)[3]) {
-  uint32_t w[3][4];
+__device__ __forceinline__ void split_bf16(f4 x, uint2 (&out)[3]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x0 = i < 2 ? a[2 * i] : b[2 * i - 4], x1 = i < 2 ? a[2 * i + 1] : b[2 * i - 3];
+  for (int n = 0; n < 3; ++n) {
+    uint32_t u[4];
 #pragma unroll
-    for (int n = 0; n < 3; ++n) {
-      const uint32_t u0 = __float_as_uint(x0), u1 = __float_as_uint(x1);
-      w[n][i] = __builtin_amdgcn_perm(u1, u0, 0x07060302u);
-      x0 -= __uint_as_float(u0 & 0xffff0000u);
-      x1 -= __uint_as_float(u1 & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(x[i]);
+    out[n] = make_uint2(__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] -= __uint_as_float(u[i] & 0xffff0000u);
   }
-#pragma unroll
-  for (int n = 0; n < 3; ++n) out[n] = __builtin_bit_cast(b8, w[n]);
 }
 
 // Whether any thread of the workgroup has `bad`; `word` is LDS that nobody uses.
@@ -404,6 +399,14 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("" ::: "memory");
 }
 
+// The waves' LDS accesses are done; loads to registers may be on their way.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Tile (tp, tq) and part of k of a workgroup.  Consecutive workgroups go to
 // the 8 XCDs in turn, each with an L2 of its own: every XCD gets a contiguous
 // run of tiles, and a run goes down groups of 8 q tiles, so that what is in
@@ -421,215 +424,80 @@ __device__ __forceinline__ void tile_of(int id, int total, int tps, int tqs, int
   *tp = id / size;
 }
 
-// WP x WQ outputs per wave.  kGated: the rows of a wave's P tile are WP / 2
-// gate rows and their up rows, so that a lane has both sums of a column.
-template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int DEPTH, int EPI, bool GATED>
-__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(const Prod a, const Epi e) {
-  constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
-  static_assert(!GATED || !PS, "the gated layer's weights are read along k");
-  typedef Operand<T, PS, BP, NW> OP;
-  typedef Operand<T, QS, BQ, NW> OQ;
-  // One array per tile: the compiler then knows that a read of one does not
-  // wait for the loads into another.
-  static_assert(DEPTH == 2 || DEPTH == 4, "buffers");
-  __shared__ __align__(16) char p0[OP::kBytes], p1[OP::kBytes], q0[OQ::kBytes], q1[OQ::kBytes];
-  __shared__ __align__(16) char p2[DEPTH > 2 ? OP::kBytes : 16], p3[DEPTH > 2 ? OP::kBytes : 16];
-  __shared__ __align__(16) char q2[DEPTH > 2 ? OQ::kBytes : 16], q3[DEPTH > 2 ? OQ::kBytes : 16];
-  char* const ps[4] = {p0, p1, p2, p3};
-  char* const qs[4] = {q0, q1, q2, q3};
-  constexpr int kFlight = OP::kLoads + OQ::kLoads;  // loads of a wave and step
+// An operand's tile walked along k, 128 bytes a step: what a lane loads where.
+template <typename T, bool S, int ROWS, int NW>
+struct Walk {
+  typedef Operand<T, S, ROWS, NW> O;
+  const char* base;
+  long long ld, kbytes, extent;  // extent: bytes from base to the operand's end
+  int lane_off, chunk;           // of a lane: its row's offset, its bytes in the row
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wp = wave % NWP, wq = wave / NWP;
-  constexpr int BC = GATED ? BP / 2 : BP;  // result columns of a tile
-  const int tps = (a.p1 - a.p0 + BC - 1) / BC, tqs = (a.q1 - a.q0 + BQ - 1) / BQ;
-  int tp, tq, split;
-  tile_of(blockIdx.x, gridDim.x, tps, tqs, &tp, &tq, &split);
-  const int cp = a.p0 + tp * BC, cq = a.q0 + tq * BQ;
-  const int step0 = split * a.steps;
-  const int all = (a.nk * (int)sizeof(T) + 127) / 128;
-  const int nsteps = min(a.steps, all - step0);
-
-  // What a lane adds to the first byte of each load's first row.
-  const int lp_ = (int)(OP::lane_row(lane) * a.ldp), cp_ = OP::lane_chunk(wave, lane);
-  const int lq_ = (int)(OQ::lane_row(lane) * a.ldq), cq_ = OQ::lane_chunk(wave, lane);
-  const char* bp = a.p + (PS ? (long long)cp * (int)sizeof(T) : cp * a.ldp);
-  const char* bq = a.q + (QS ? (long long)cq * (int)sizeof(T) : cq * a.ldq);
-  const long long kbytes = (long long)a.nk * (int)sizeof(T);
-
-  auto stage = [&](int s, char* lp, char* lq) __attribute__((always_inline)) {
-    // C: bytes of k before this step; S: rows of k before it.
-    const int step = step0 + s;
-    const bool none = s >= nsteps;  // loads nothing: the loop runs ahead of its end
-    const long long at = (long long)step * 128, row = (long long)step * OP::kStep;
-    const int left = (int)min(kbytes - at, 128LL);  // C: bytes of k in this step
-    const long long op = PS ? row * a.ldp : at, oq = QS ? row * a.ldq : at;
-    const long long ep = PS ? (a.kp - 1 - row) * a.ldp + (long long)(a.colsp - cp) * (int)sizeof(T)
-                            : (a.np - 1 - cp) * a.ldp + kbytes - at;
-    const long long eq = QS ? (a.kq - 1 - row) * a.ldq + (long long)(a.colsq - cq) * (int)sizeof(T)
-                            : (a.nq - 1 - cq) * a.ldq + kbytes - at;
-    const __amdgpu_buffer_rsrc_t rq = descriptor(bq + oq, none ? 0 : eq), rp = descriptor(bp + op, none ? 0 : ep);
-    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(bp + op + a.p2 * a.ldp, none ? 0 : ep) : rp;
-#pragma unroll
-    for (int j = 0; j < OP::kLoads; ++j) {
-      int r = OP::first(wave, j);
-      const bool up = GATED && r % WP >= WP / 2;
-      if (GATED) r = r / WP * (WP / 2) + r % (WP / 2);
-      int v = lp_ + (cp_ ^ OP::chunk_delta(j)) + (int)(r * a.ldp);
-      if (!PS) v = cp_ >= left ? (int)0x80000000 : v;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(up ? rp2 : rp, (lds_void*)(lp + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < OQ::kLoads; ++j) {
-      int v = lq_ + (cq_ ^ OQ::chunk_delta(j)) + (int)(OQ::first(wave, j) * a.ldq);
-      if (!QS) v = cq_ >= left ? (int)0x80000000 : v;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lq + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
-    }
-  };
-
-  f4 acc[FP][FQ];
-#pragma unroll
-  for (int i = 0; i < FP; ++i)
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-
-  if constexpr (sizeof(T) == 4) {
-    // fp32 as three bf16 parts (split_bf16): six products of them instead of
-    // fp32's own matrix instruction, which has 1/16 of bf16's rate.  The step's
-    // 32 k's are one bf16 instruction, elements 0..3 of a lane from its first
-    // half and 4..7 from its second.  An infinity's lower parts are NaN, so a
-    // tile whose sums are not all finite is computed again in fp32.
-    const int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
-    auto step = [&](const char* lp, const char* lq, auto split) __attribute__((always_inline)) {
-      if constexpr (decltype(split)::value) {
-        b8 fq[FQ][3];
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) split_bf16(OQ::frag(lq, rq_, j, 0), OQ::frag(lq, rq_, j, 1), fq[j]);
-#pragma unroll
-        for (int i = 0; i < FP; ++i) {
-          b8 fp[3];
-          split_bf16(OP::frag(lp, rp_, i, 0), OP::frag(lp, rp_, i, 1), fp);
-#pragma unroll
-          for (int n = 0; n < 6; ++n) {  // smallest first
-            constexpr int kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0};
-#pragma unroll
-            for (int j = 0; j < FQ; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[kA[n]], fq[j][kB[n]], acc[i][j], 0, 0, 0);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-          for (int i = 0; i < FP; ++i)
-#pragma unroll
-            for (int j = 0; j < FQ; ++j)
-              acc[i][j] = Num<T>::mma(OP::frag(lp, rp_, i, kk), OQ::frag(lq, rq_, j, kk), acc[i][j]);
-      }
-    };
-    auto loop = [&](auto split) __attribute__((always_inline)) {
-#pragma unroll
-      for (int b = 0; b < DEPTH - 1; ++b) stage(b, ps[b], qs[b]);
-      for (int s = 0; s < nsteps; s += DEPTH) {
-#pragma unroll
-        for (int b = 0; b < DEPTH; ++b) {
-          if (s + b >= nsteps) break;
-          wait_and_meet<(DEPTH - 2) * kFlight>();
-          stage(s + b + DEPTH - 1, ps[(b + DEPTH - 1) % DEPTH], qs[(b + DEPTH - 1) % DEPTH]);
-          step(ps[b], qs[b], split);
-        }
-      }
-      wait_and_meet<0>();
-    };
-    loop(std::true_type());
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < FP; ++i)
-#pragma unroll
-      for (int j = 0; j < FQ; ++j)
-#pragma unroll
-        for (int n = 0; n < 4; ++n) bad |= !(fabsf(acc[i][j][n]) < INFINITY);
-    if (any_of_group(bad, reinterpret_cast<int*>(p0))) {
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-      loop(std::false_type());
-    }
-  } else {
-    struct Frags {
-      typename Num<T>::Frag p[FP], q[FQ];
-    };
-    int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
-    auto read = [&](Frags& f, const char* lp, const char* lq, int kk) __attribute__((always_inline)) {
-      // One register each: the fragments' addresses are made from it again
-      // every time (the registers are for the sums and two sets of fragments).
-      asm volatile("" : "+v"(rp_), "+v"(rq_));
-#pragma unroll
-      for (int j = 0; j < FQ; ++j) f.q[j] = OQ::frag(lq, rq_, j, kk);
-#pragma unroll
-      for (int i = 0; i < FP; ++i) f.p[i] = OP::frag(lp, rp_, i, kk);
-    };
-    auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < FP; ++i)
-#pragma unroll
-        for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
-    };
-    // LDS reads, and a step's loads, one by one between the products.
-    auto interleave = [](auto loads_) __attribute__((always_inline)) {
-      constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ * (sizeof(T) == 4 ? 4 : 1);
-      constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
-      constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        if (i < reads) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-        }
-        if (i < loads) {
-          __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-        }
-      }
-      constexpr int rest = mmas - per * (reads + loads);
-      if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
-    };
-    // A step: the first half's fragments are in f0.  Reads its second half
-    // under the first half's products; then everyone's reads of this buffer are
-    // done and everyone's loads of the next have landed: the step that is DEPTH
-    // further on is sent for, and the next step's first half is read under the
-    // second half's products.
-    Frags f0, f1;
-    auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) __attribute__((always_inline)) {
-      read(f1, lp, lq, 1);
-      multiply(f0);
-      interleave(std::integral_constant<int, 0>());
-      __builtin_amdgcn_sched_barrier(0);
-      wait_and_meet<(DEPTH - 2) * kFlight>();
-      stage(s + DEPTH, lp, lq);
-      read(f0, next_p, next_q, 0);
-      multiply(f1);
-      interleave(std::integral_constant<int, kFlight>());
-      __builtin_amdgcn_sched_barrier(0);
-    };
-
-#pragma unroll
-    for (int b = 0; b < DEPTH; ++b) stage(b, ps[b], qs[b]);
-    wait_and_meet<(DEPTH - 1) * kFlight>();
-    read(f0, p0, q0, 0);
-    int s = 0;
-    for (; s + DEPTH <= nsteps; s += DEPTH) {
-#pragma unroll
-      for (int b = 0; b < DEPTH; ++b) body(s + b, ps[b], qs[b], ps[(b + 1) % DEPTH], qs[(b + 1) % DEPTH]);
-    }
-#pragma unroll
-    for (int b = 0; b < DEPTH - 1; ++b)
-      if (s + b < nsteps) body(s + b, ps[b], qs[b], ps[b + 1], qs[b + 1]);
-    wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
+  // first: the tile's first row of `rows` (C) or column of `cols` stored (S);
+  // krows: an S operand's rows.  swizzled: the lanes' chunks in the order that
+  // LDS wants them, for loads that go there.
+  __device__ __forceinline__ Walk(const char* p, long long ld_, int first, int rows, int cols, int nk, int krows,
+                                  int wave, int lane, bool swizzled)
+      : ld(ld_), kbytes((long long)nk * O::kS) {
+    base = p + (S ? (long long)first * O::kS : first * ld);
+    extent = S ? (krows - 1) * ld + (long long)(cols - first) * O::kS : (rows - 1 - first) * ld + kbytes;
+    lane_off = (int)(O::lane_row(lane) * ld);
+    chunk = swizzled ? O::lane_chunk(wave, lane) : lane % O::kPerRow * 16;
   }
 
-  // ---- epilogue: acc[i][j] holds p = 16 i + 4 g + 0..3 of q = 16 j + lane % 16
+  // The tile's first byte in a step, and from there to the operand's end.
+  __device__ __forceinline__ long long before(int step) const {
+    return S ? (long long)step * O::kStep * ld : (long long)step * 128;
+  }
+  // Bytes of k that a C operand has in this step.
+  __device__ __forceinline__ int left(int step) const { return (int)min(kbytes - (long long)step * 128, 128LL); }
+
+  // Offset of load j's 16 bytes; row: the load's first in the tile.
+  __device__ __forceinline__ int offset(int row, int delta, int left) const {
+    const int v = lane_off + (chunk ^ delta) + (int)(row * ld);
+    return !S && chunk >= left ? (int)0x80000000 : v;
+  }
+};
+
+// A step's descriptor, `rows_on` rows further on; none: it holds nothing.
+template <typename W>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const W& w, int step, bool none, long long rows_on = 0) {
+  const long long before = w.before(step);
+  return descriptor(w.base + before + rows_on * w.ld, none ? 0 : w.extent - before);
+}
+
+// The weight row of a gated tile's row: a wave's WP rows are WP / 2 gate rows
+// and, from the same first one, their up rows, so that a lane has both sums.
+template <int WP>
+__device__ __forceinline__ int gated_row(int r) { return r / WP * (WP / 2) + r % (WP / 2); }
+template <int WP>
+__device__ __forceinline__ bool gated_up(int r) { return r % WP >= WP / 2; }
+
+// Where a workgroup's tile lies.
+struct Place {
+  int tp, cp, cq, split, step0, nsteps;
+};
+
+template <int BC, int BQ, int S>
+__device__ __forceinline__ Place place_of(const Prod& a) {
+  Place t;
+  int tq;
+  tile_of(blockIdx.x, gridDim.x, (a.p1 - a.p0 + BC - 1) / BC, (a.q1 - a.q0 + BQ - 1) / BQ, &t.tp, &tq, &t.split);
+  t.cp = a.p0 + t.tp * BC;
+  t.cq = a.q0 + tq * BQ;
+  t.step0 = t.split * a.steps;
+  t.nsteps = min(a.steps, (a.nk * S + 127) / 128 - t.step0);
+  return t;
+}
+
+constexpr int kRoomBytes = 16384;
+
+// What becomes of a wave's sums: acc[i][j] holds p = 16 i + 4 g + 0..3 of
+// q = 16 j + lane % 16.  room: 16 KB of LDS for this wave alone.
+template <typename T, int WP, int WQ, int NWP, int EPI, bool GATED>
+__device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const Place& at, f4 (&acc)[WP / 16][WQ / 16],
+                                            f4* room, int lane, int wp, int wq) {
+  constexpr int FP = WP / 16, FQ = WQ / 16;
+  const int tp = at.tp, cp = at.cp, cq = at.cq, split = at.split;
   const int g = lane >> 4, c = lane & 15;
   if constexpr (EPI == kStats) {
     const int q_first = cq + wq * WQ + c;
@@ -665,15 +533,9 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
     // 16 rows' 32 bytes each, and memory wants whole lines (stored as they
     // are, 2.4 times the result's bytes were written to HBM).  Row q's quad p
     // lies at p ^ (q % 16), free of conflicts both ways.
-    constexpr int kRoom = 4 * OP::kBytes / NW, kRows = kRoom / (WP * 4) < WQ ? kRoom / (WP * 4) : WQ;
+    constexpr int kRows = kRoomBytes / (WP * 4) < WQ ? kRoomBytes / (WP * 4) : WQ;
     constexpr int kQuads = WP / 4, kOut = GATED ? kQuads / 2 : kQuads;  // of a row; that one emit covers
-    static_assert(OP::kBytes == OQ::kBytes && OP::kBytes % kRoom == 0, "a wave's room lies in one tile");
-    constexpr int kPer = OP::kBytes / kRoom;
-    char* const tiles[4] = {p0, p1, q0, q1};
-    f4* room = reinterpret_cast<f4*>(tiles[0] + wave % kPer * kRoom);
-#pragma unroll
-    for (int t = 1; t < 4; ++t)
-      if (wave / kPer == t) room = reinterpret_cast<f4*>(tiles[t] + wave % kPer * kRoom);
+    static_assert(kQuads >= 16 && kRows % 16 == 0, "the XOR stays within a row");
 #pragma unroll
     for (int first = 0; first < WQ; first += kRows) {
 #pragma unroll
@@ -707,6 +569,313 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
       }
     }
   }
+}
+
+// 16-bit products.  WP x WQ outputs per wave, DEPTH steps in LDS.
+template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int DEPTH, int EPI, bool GATED>
+__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(const Prod a, const Epi e) {
+#ifdef __HIP_DEVICE_COMPILE__  // the host pass, which only needs the name, gives up on the body without a word
+  constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
+  static_assert(!GATED || !PS, "the gated layer's weights are read along k");
+  typedef Operand<T, PS, BP, NW> OP;
+  typedef Operand<T, QS, BQ, NW> OQ;
+  // One array per tile: the compiler then knows that a read of one does not
+  // wait for the loads into another.
+  static_assert(DEPTH == 2 || DEPTH == 4, "buffers");
+  __shared__ __align__(16) char p0[OP::kBytes], p1[OP::kBytes], q0[OQ::kBytes], q1[OQ::kBytes];
+  __shared__ __align__(16) char p2[DEPTH > 2 ? OP::kBytes : 16], p3[DEPTH > 2 ? OP::kBytes : 16];
+  __shared__ __align__(16) char q2[DEPTH > 2 ? OQ::kBytes : 16], q3[DEPTH > 2 ? OQ::kBytes : 16];
+  char* const ps[4] = {p0, p1, p2, p3};
+  char* const qs[4] = {q0, q1, q2, q3};
+  constexpr int kFlight = OP::kLoads + OQ::kLoads;  // loads of a wave and step
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wp = wave % NWP, wq = wave / NWP;
+  const Place t = place_of<GATED ? BP / 2 : BP, BQ, sizeof(T)>(a);
+  const int nsteps = t.nsteps;
+  const Walk<T, PS, BP, NW> walk_p(a.p, a.ldp, t.cp, a.np, a.colsp, a.nk, a.kp, wave, lane, true);
+  const Walk<T, QS, BQ, NW> walk_q(a.q, a.ldq, t.cq, a.nq, a.colsq, a.nk, a.kq, wave, lane, true);
+
+  auto stage = [&](int s, char* lp, char* lq) __attribute__((always_inline)) {
+    const int step = t.step0 + s;
+    const bool none = s >= nsteps;  // loads nothing: the loop runs ahead of its end
+    const __amdgpu_buffer_rsrc_t rq = descriptor(walk_q, step, none), rp = descriptor(walk_p, step, none);
+    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(walk_p, step, none, a.p2) : rp;
+    const int left = walk_p.left(step);
+#pragma unroll
+    for (int j = 0; j < OP::kLoads; ++j) {
+      const int r = OP::first(wave, j);
+      const int v = walk_p.offset(GATED ? gated_row<WP>(r) : r, OP::chunk_delta(j), left);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && gated_up<WP>(r) ? rp2 : rp,
+                                               (lds_void*)(lp + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < OQ::kLoads; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lq + (wave + j * NW) * 1024), 16,
+                                               walk_q.offset(OQ::first(wave, j), OQ::chunk_delta(j), left), 0, 0, 0);
+  };
+
+  f4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+  struct Frags {
+    typename Num<T>::Frag p[FP], q[FQ];
+  };
+  int rp_ = OP::lane_base(lane, wp * WP), rq_ = OQ::lane_base(lane, wq * WQ);
+  auto read = [&](Frags& f, const char* lp, const char* lq, int kk) __attribute__((always_inline)) {
+    // One register each: the fragments' addresses are made from it again
+    // every time (the registers are for the sums and two sets of fragments).
+    asm volatile("" : "+v"(rp_), "+v"(rq_));
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) f.q[j] = OQ::frag(lq, rq_, j, kk);
+#pragma unroll
+    for (int i = 0; i < FP; ++i) f.p[i] = OP::frag(lp, rp_, i, kk);
+  };
+  auto multiply = [&](const Frags& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
+  };
+  // LDS reads, and a step's loads, one by one between the products.
+  auto interleave = [](auto loads_) __attribute__((always_inline)) {
+    constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ;
+    constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
+    constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      if (i < reads) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+      }
+      if (i < loads) {
+        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+      }
+    }
+    constexpr int rest = mmas - per * (reads + loads);
+    if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
+  };
+  // A step: the first half's fragments are in f0.  Reads its second half
+  // under the first half's products; then everyone's reads of this buffer are
+  // done and everyone's loads of the next have landed: the step that is DEPTH
+  // further on is sent for, and the next step's first half is read under the
+  // second half's products.
+  Frags f0, f1;
+  auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) __attribute__((always_inline)) {
+    read(f1, lp, lq, 1);
+    multiply(f0);
+    interleave(std::integral_constant<int, 0>());
+    __builtin_amdgcn_sched_barrier(0);
+    wait_and_meet<(DEPTH - 2) * kFlight>();
+    stage(s + DEPTH, lp, lq);
+    read(f0, next_p, next_q, 0);
+    multiply(f1);
+    interleave(std::integral_constant<int, kFlight>());
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+#pragma unroll
+  for (int b = 0; b < DEPTH; ++b) stage(b, ps[b], qs[b]);
+  wait_and_meet<(DEPTH - 1) * kFlight>();
+  read(f0, p0, q0, 0);
+  int s = 0;
+  for (; s + DEPTH <= nsteps; s += DEPTH) {
+#pragma unroll
+    for (int b = 0; b < DEPTH; ++b) body(s + b, ps[b], qs[b], ps[(b + 1) % DEPTH], qs[(b + 1) % DEPTH]);
+  }
+#pragma unroll
+  for (int b = 0; b < DEPTH - 1; ++b)
+    if (s + b < nsteps) body(s + b, ps[b], qs[b], ps[b + 1], qs[b + 1]);
+  wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
+
+  constexpr int kPer = OP::kBytes / kRoomBytes;  // waves' rooms in a tile
+  static_assert(OP::kBytes == OQ::kBytes && kPer * 4 >= NW, "a room for each wave");
+  char* room = p0;
+#pragma unroll
+  for (int b = 1; b < 4; ++b)
+    if (wave / kPer == b) room = b == 1 ? p1 : b == 2 ? q0 : q1;
+  finish_tile<T, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, reinterpret_cast<f4*>(room + wave % kPer * kRoomBytes), lane,
+                                          wp, wq);
+#endif
+}
+
+// ---- fp32 products: three bf16 parts of each number, six products of them,
+// instead of fp32's own matrix instruction, which has 1/16 of bf16's rate.
+// The parts are made once per workgroup, between memory and LDS (made where
+// the fragments are read, every number is split by two to four waves, and
+// splitting takes as long as multiplying): a step's 32 k's go to registers, a
+// step ahead, then as three tiles of bf16 to LDS, double-buffered.
+//   C: rows of 64 bytes, chunk c (16 bytes, 8 k's) of row r at c ^ ((r >> 2) & 3).
+//   S: rows along p or q as for 16-bit types, read transposed.
+template <bool S, int ROWS, int NW>
+struct Planes {
+  typedef Operand<float, S, ROWS, NW> O;             // of the loads
+  typedef Operand<__bf16, S, ROWS, NW> R;            // of an S tile's rows in LDS
+  static constexpr int kPlane = ROWS * 64, kBytes = 3 * kPlane, kLoads = O::kLoads;
+
+  // Where a lane's four numbers of load j go in a plane.
+  static __device__ __forceinline__ int lane_write(int wave, int lane) {
+    const int r = O::first(wave, 0) + O::lane_row(lane), c = lane % O::kPerRow;  // c: four numbers
+    if (!S) return r * 64 + (((c >> 1) ^ ((r >> 2) & 3)) << 4) + (c & 1) * 8;
+    return r * R::kRowBytes + (((c >> 1) ^ swizzle(r)) << 4) + (c & 1) * 8;
+  }
+  static constexpr __device__ int swizzle(int r) { return 2 * ((r & 3) | (((r >> 3) & 1) << 2)); }
+  static __device__ __forceinline__ int write_at(int base, int j) {
+    constexpr int kRow = S ? ROWS * 2 : 64;
+    return (S ? base ^ (swizzle(j * NW * O::kRowsPer) << 4) : base) + j * NW * O::kRowsPer * kRow;
+  }
+
+  static __device__ __forceinline__ int lane_read(int lane, int at) {
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (S) return R::lane_base(lane, at);
+    else return (at + i) * 64 + ((g ^ ((i >> 2) & 3)) << 4);
+  }
+  static __device__ __forceinline__ b8 frag(const char* plane, int base, int f) {
+    if constexpr (S) return R::frag(plane, base, f, 0);
+    else return *reinterpret_cast<const b8*>(plane + base + f * 1024);
+  }
+};
+
+template <bool PS, bool QS, int BP, int BQ, int WP, int WQ, int EPI, bool GATED>
+__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel(const Prod a, const Epi e) {
+#ifdef __HIP_DEVICE_COMPILE__
+  constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
+  static_assert(!GATED || !PS, "the gated layer's weights are read along k");
+  typedef Planes<PS, BP, NW> LP;
+  typedef Planes<QS, BQ, NW> LQ;
+  constexpr int kBuffer = LP::kBytes + LQ::kBytes;
+  constexpr int kLds = 2 * kBuffer > NW * kRoomBytes ? 2 * kBuffer : NW * kRoomBytes;
+  __shared__ __align__(16) char lds[kLds];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wp = wave % NWP, wq = wave / NWP;
+  const Place t = place_of<GATED ? BP / 2 : BP, BQ, 4>(a);
+  const Walk<float, PS, BP, NW> walk_p(a.p, a.ldp, t.cp, a.np, a.colsp, a.nk, a.kp, wave, lane, false);
+  const Walk<float, QS, BQ, NW> walk_q(a.q, a.ldq, t.cq, a.nq, a.colsq, a.nk, a.kq, wave, lane, false);
+
+  f4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+
+  // Numbers on their way: load j < LP::kLoads of P, then those of Q.
+  constexpr int kLoads = LP::kLoads + LQ::kLoads;
+  f4 ahead[kLoads];
+  const int write_p = LP::lane_write(wave, lane), write_q = LQ::lane_write(wave, lane);
+  const int read_p = LP::lane_read(lane, wp * WP), read_q = LQ::lane_read(lane, wq * WQ);
+  auto load = [&](int s, int j) __attribute__((always_inline)) {
+    const int step = t.step0 + s, left = walk_p.left(step);
+    const bool none = s >= t.nsteps;
+    if (j < LP::kLoads) {
+      const int r = LP::O::first(wave, j);
+      const __amdgpu_buffer_rsrc_t rsrc = descriptor(walk_p, step, none, GATED && gated_up<WP>(r) ? a.p2 : 0);
+      const int v = walk_p.offset(GATED ? gated_row<WP>(r) : r, 0, left);
+      ahead[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, v, 0, 0));
+    } else {
+      const int v = walk_q.offset(LQ::O::first(wave, j - LP::kLoads), 0, left);
+      ahead[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(descriptor(walk_q, step, none), v, 0, 0));
+    }
+  };
+  auto put = [&](char* buffer, int j) __attribute__((always_inline)) {
+    const bool is_p = j < LP::kLoads;
+    char* o = is_p ? buffer + LP::write_at(write_p, j) : buffer + LP::kBytes + LQ::write_at(write_q, j - LP::kLoads);
+    uint2 w[3];
+    split_bf16(ahead[j], w);
+#pragma unroll
+    for (int n = 0; n < 3; ++n) *reinterpret_cast<uint2*>(o + n * (is_p ? LP::kPlane : LQ::kPlane)) = w[n];
+  };
+
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) load(0, j);
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    put(lds, j);
+    load(1, j);
+  }
+  meet();
+  for (int s = 0; s < t.nsteps; ++s) {
+    const char* now = lds + (s & 1) * kBuffer;
+    char* next = lds + (~s & 1) * kBuffer;
+    b8 fq[FQ][3];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+      for (int n = 0; n < 3; ++n) fq[j][n] = LQ::frag(now + LP::kBytes + n * LQ::kPlane, read_q, j);
+#pragma unroll
+    for (int i = 0; i < FP; ++i) {
+      b8 fp[3];
+#pragma unroll
+      for (int n = 0; n < 3; ++n) fp[n] = LP::frag(now + n * LP::kPlane, read_p, i);
+#pragma unroll
+      for (int n = 0; n < 6; ++n) {  // smallest first
+        constexpr int kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int j = 0; j < FQ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[kA[n]], fq[j][kB[n]], acc[i][j], 0, 0, 0);
+      }
+      // The next step's numbers, some after each of these products.
+#pragma unroll
+      for (int j = i * kLoads / FP; j < (i + 1) * kLoads / FP; ++j) {
+        put(next, j);
+        load(s + 2, j);
+      }
+    }
+    meet();
+  }
+
+  // An infinity's lower parts are NaN: a tile whose sums are not all finite is
+  // computed again with fp32's own instruction, from fp32 tiles in LDS.
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) bad |= !(fabsf(acc[i][j][n]) < INFINITY);
+  if (any_of_group(bad, reinterpret_cast<int*>(lds))) {
+    typedef Operand<float, PS, BP, NW> OP;
+    typedef Operand<float, QS, BQ, NW> OQ;
+    const Walk<float, PS, BP, NW> again_p(a.p, a.ldp, t.cp, a.np, a.colsp, a.nk, a.kp, wave, lane, true);
+    const Walk<float, QS, BQ, NW> again_q(a.q, a.ldq, t.cq, a.nq, a.colsq, a.nk, a.kq, wave, lane, true);
+    const int base_p = OP::lane_base(lane, wp * WP), base_q = OQ::lane_base(lane, wq * WQ);
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < t.nsteps; ++s) {
+      const int step = t.step0 + s, left = again_p.left(step);
+#pragma unroll
+      for (int j = 0; j < OP::kLoads; ++j) {
+        const int r = OP::first(wave, j);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            descriptor(again_p, step, false, GATED && gated_up<WP>(r) ? a.p2 : 0), (lds_void*)(lds + (wave + j * NW) * 1024), 16,
+            again_p.offset(GATED ? gated_row<WP>(r) : r, OP::chunk_delta(j), left), 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < OQ::kLoads; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            descriptor(again_q, step, false), (lds_void*)(lds + OP::kBytes + (wave + j * NW) * 1024), 16,
+            again_q.offset(OQ::first(wave, j), OQ::chunk_delta(j), left), 0, 0, 0);
+      wait_and_meet<0>();
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+          for (int j = 0; j < FQ; ++j)
+            acc[i][j] = Num<float>::mma(OP::frag(lds, base_p, i, kk), OQ::frag(lds + OP::kBytes, base_q, j, kk),
+                                        acc[i][j]);
+      wait_and_meet<0>();
+    }
+  }
+  finish_tile<float, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, reinterpret_cast<f4*>(lds + wave * kRoomBytes), lane, wp,
+                                              wq);
+#endif
 }
 
 }  // namespace dense

@@ -329,41 +329,48 @@ static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restri
 
 // A product's tiles and parts of k.
 struct Cut {
-  int big;  // 256 x 256 tiles of 8 waves, else 128 x 128 of 4
+  int big;  // large tiles of 8 waves: 256 x 256, fp32 256 x 128; else 128 x 128
   int main_p, main_q;  // large tiles along one axis (0: all), the rest in small ones
   int splits, steps;
   size_t part_bytes;
   long long ldpart;
 };
 
-inline long long tiles_of(int np, int nq, bool gated, int edge) {
-  return (long long)ceil_div(np, gated ? edge / 2 : edge) * ceil_div(nq, edge);
-}
+// Results of a tile along p and q.
+template <typename T>
+struct Edge {
+  static constexpr int p(bool big, bool gated) { return (big ? 256 : 128) / (gated ? 2 : 1); }
+  static constexpr int q(bool big) { return big && sizeof(T) == 2 ? 256 : 128; }
+  static constexpr int slots(bool big) { return big && sizeof(T) == 4 ? 4 : 2; }  // waves along p
+  static long long tiles(int np, int nq, bool gated, bool big) {
+    return (long long)ceil_div(np, p(big, gated)) * ceil_div(nq, q(big));
+  }
+};
 
 // The cut that should take the least time: the steps in a row of the busiest
-// CU, times what one takes.  A CU holds one large tile or two small ones; two
-// small ones hide each other's waits.  Measured per step on whole products (k
-// of 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.6 to 0.75
-// us, two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32: 1.6,
-// 2.75, 4.2 to 4.7.  Parts of k are written and read once in fp32 (5 TB/s) and
-// take a second kernel.  Against the best of all measured cuts of ten shapes
-// the choice loses 0 to 12 %, against one fixed rule (256 workgroups) it gains
-// up to 1.4 times (1024 x 4096 -> 1024 in fp32: 57 us, 64 with one workgroup per
-// CU).
+// CU, times what one takes.  A CU holds one tile, or two small 16-bit ones,
+// which hide each other's waits.  Measured per step on whole products (k of
+// 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.6 to 0.75 us,
+// two 1.15, a large one 1.4 to 1.7 (four small ones' work).  Parts of k are
+// written and read once in fp32 (5 TB/s) and take a second kernel.  Against
+// the best of all measured cuts of ten shapes the choice loses 0 to 12 %; one
+// fixed rule (256 workgroups) lost up to 1.4 times.
 // A last round of large tiles that would leave most CUs idle goes in small ones
 // (1999 rows to 50001 classes: 6.1 rounds).  rows_alike: not along q.
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
-  const double one = sizeof(T) == 4 ? 1.85 : 0.66, two = sizeof(T) == 4 ? 2.75 : 1.15, large = sizeof(T) == 4 ? 4.5 : 1.6;
+  constexpr bool f32 = sizeof(T) == 4;
+  const double one = f32 ? 1.2 : 0.66, two = 1.15, large = f32 ? 2.2 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
   auto small_rounds = [&](long long groups) {
+    if (f32) return (groups + 255) / 256 * one;
     const long long rest = groups % 512;
     return groups / 512 * two + (rest > 256 ? two : rest ? one : 0.);
   };
   Cut best = {};
   double least = 1e300;
   for (int big = 0; big < 2; ++big) {
-    const long long tiles = tiles_of(np, nq, gated, big ? 256 : 128);
+    const long long tiles = Edge<T>::tiles(np, nq, gated, big);
     for (int n = 1; n <= 32 && (n == 1 || (n <= all / 2 && tiles * n <= 1024)); ++n) {
       const int steps = ceil_div(all, n), splits = ceil_div(all, steps);
       const long long groups = tiles * splits;
@@ -376,13 +383,14 @@ Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
       best.steps = steps;
     }
   }
-  const int width = gated ? 128 : 256, tps = ceil_div(np, width), tqs = ceil_div(nq, 256);
+  const int wide = Edge<T>::p(true, gated), high = Edge<T>::q(true), tps = ceil_div(np, wide), tqs = ceil_div(nq, high);
   const long long rounds = (long long)tps * tqs / 256;
   for (int axis = 0; axis < (rows_alike ? 1 : 2) && rounds > 0; ++axis) {
     const int mine = axis ? tqs : tps, other = axis ? tps : tqs;
     const int main = (int)(rounds * 256 / other);
     if (main < 1 || main >= mine) continue;
-    const long long tail = axis ? tiles_of(np, nq - main * 256, gated, 128) : tiles_of(np - main * width, nq, gated, 128);
+    const long long tail = axis ? Edge<T>::tiles(np, nq - main * high, gated, false)
+                                : Edge<T>::tiles(np - main * wide, nq, gated, false);
     const double t = all * (((long long)main * other + 255) / 256 * large + small_rounds(tail)) + 4.;
     if (t >= least) continue;
     least = t;
@@ -404,21 +412,27 @@ hipError_t launch_tiles(Prod a, const Epi& e, bool big, int p0, int p1, int q0, 
   a.q0 = q0;
   a.q1 = q1;
   LaunchTimer timer;
-  const dim3 grid((unsigned)tiles_of(p1 - p0, q1 - q0, GATED, big ? 256 : 128) * a.splits);
-  if (big)
-    return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, 2, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
-  if (grid.x <= 256)  // one workgroup per CU: its LDS holds four steps (1024 x 4096 -> 1024 bf16: 45 us, with four 39)
-    return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 4, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
-  return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 2, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+  const dim3 grid((unsigned)(Edge<T>::tiles(p1 - p0, q1 - q0, GATED, big) * a.splits));
+  if constexpr (sizeof(T) == 4) {
+    if (big)
+      return timed_launch(&timer, product_f32_kernel<PS, QS, 256, 128, 64, 64, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
+    return timed_launch(&timer, product_f32_kernel<PS, QS, 128, 128, 64, 32, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
+  } else {
+    if (big)
+      return timed_launch(&timer, product_kernel<T, PS, QS, 256, 256, 128, 64, 2, EPI, GATED>, grid, dim3(512), 0u, st, a, e);
+    if (grid.x <= 256)  // one workgroup per CU: its LDS holds four steps (1024 x 4096 -> 1024 bf16: 45 us, with four 39)
+      return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 4, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+    return timed_launch(&timer, product_kernel<T, PS, QS, 128, 128, 64, 64, 2, EPI, GATED>, grid, dim3(256), 0u, st, a, e);
+  }
 }
 
 template <typename T, bool PS, bool QS, int EPI, bool GATED>
 hipError_t launch_product(Prod a, const Epi& e, const Cut& c, hipStream_t st) {
-  const int p = c.main_p * (GATED ? 128 : 256), q = c.main_q * 256;
+  const int p = c.main_p * Edge<T>::p(true, GATED), q = c.main_q * Edge<T>::q(true);
   if (!p && !q) return launch_tiles<T, PS, QS, EPI, GATED>(a, e, c.big, 0, a.np, 0, a.nq, st);
   const hipError_t err = launch_tiles<T, PS, QS, EPI, GATED>(a, e, true, 0, p ? p : a.np, 0, q ? q : a.nq, st);
   if (err != hipSuccess) return err;
-  if (p) a.slot0 = 2 * c.main_p;
+  if (p) a.slot0 = Edge<T>::slots(true) * c.main_p;
   return launch_tiles<T, PS, QS, EPI, GATED>(a, e, false, p, a.np, q, a.nq, st);
 }
 
@@ -455,11 +469,14 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   return err != hipSuccess ? err : finish<T, EPI>(a.np, a.nq, e, c, part, st);
 }
 
-// Slots of a product that is not split: one per wave along p, 2 in a tile (the
-// same for every row, so none of its rows may go in tiles of another size).
-inline int stat_slots(const Cut& c, int np) {
-  if (c.main_p) return 2 * c.main_p + 2 * ceil_div(np - c.main_p * 256, 128);
-  return 2 * ceil_div(np, c.big ? 256 : 128);
+// Slots of a product that is not split: one per wave along p (the same for
+// every row, so none of its rows may go in tiles of another size).
+template <typename T>
+int stat_slots(const Cut& c, int np) {
+  typedef Edge<T> E;
+  if (c.main_p)
+    return E::slots(true) * c.main_p + E::slots(false) * ceil_div(np - c.main_p * E::p(true, false), E::p(false, false));
+  return E::slots(c.big) * ceil_div(np, E::p(c.big, false));
 }
 
 // A forward product: the tiles, or for few rows the kernel that streams the
@@ -480,7 +497,7 @@ struct Forward : Cut {
     few = nq <= kFewRows<T>;
     if (!few) {
       static_cast<Cut&>(*this) = cut_of<T>(np, nq, pad16<T>(nk), gated, rows_alike);
-      slots = splits > 1 ? loss_slots(np) : stat_slots(*this, np);
+      slots = splits > 1 ? loss_slots(np) : stat_slots<T>(*this, np);
       return;
     }
     // A wave's 16 rows (32 past 8 rows of x and where there are many, whose
