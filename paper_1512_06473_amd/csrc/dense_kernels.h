@@ -351,7 +351,8 @@ struct Edge {
 // CU, times what one takes.  A CU holds one tile, or two small 16-bit ones,
 // which hide each other's waits.  Measured per step on whole products (k of
 // 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.6 to 0.75 us,
-// two 1.15, a large one 1.4 to 1.7 (four small ones' work).  Parts of k are
+// two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32 1.4, a large
+// one (twice the work) 2.4 to 2.65.  Parts of k are
 // written and read once in fp32 (5 TB/s) and take a second kernel.  Against
 // the best of all measured cuts of ten shapes the choice loses 0 to 12 %; one
 // fixed rule (256 workgroups) lost up to 1.4 times.
@@ -360,7 +361,7 @@ struct Edge {
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
   constexpr bool f32 = sizeof(T) == 4;
-  const double one = f32 ? 1.2 : 0.66, two = 1.15, large = f32 ? 2.2 : 1.6;
+  const double one = f32 ? 1.4 : 0.66, two = 1.15, large = f32 ? 2.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
   auto small_rounds = [&](long long groups) {
     if (f32) return (groups + 255) / 256 * one;
