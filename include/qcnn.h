@@ -368,7 +368,7 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
  * element.  Rows of whole 16 bytes at 16-byte aligned addresses are read in
  * place; otherwise x and w are first copied into the workspace.
  * Limits: N <= 2^21; C_s, C_t (2 C_t of the gated layer) and strides <= 2^20;
- * no more than 2^23 tiles of 128 x 128 in any of the products
+ * no more than 2^22 tiles of 128 x 128 in any of the products
  * (QCNN_ERR_UNSUPPORTED past them).  Sizes are at least 1.
  * Workspace: with workspace_bytes NULL the library's per-stream workspace is
  * used.  With workspace NULL and workspace_bytes not NULL the call only

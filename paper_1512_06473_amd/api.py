@@ -649,6 +649,12 @@ def _vector(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, n: int, de
     return t.data_ptr()
 
 
+# The stream's handle without a Stream object around it (2 us of a call's 10 on
+# the host), where this torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _dense_call(entry: str, device, args) -> None:
     """One call on the device's current stream.  A call that is being captured
     into a graph gets a workspace of its own from torch, which the graph's
@@ -658,7 +664,7 @@ def _dense_call(entry: str, device, args) -> None:
     if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
             return _dense_call(entry, device, args)
-    stream = torch.cuda.current_stream(device).cuda_stream
+    stream = _raw_stream(device.index)
     if not torch.cuda.is_current_stream_capturing():
         return check(f(*args, None, None, stream), entry)
     size = ctypes.c_size_t(0)

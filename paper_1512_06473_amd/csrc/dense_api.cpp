@@ -8,9 +8,9 @@ namespace {
 
 using qcnn::dense::DenseCall;
 
-constexpr int kMaxRows = 1 << 21;    // 64 rows per block of a grid's second axis
-constexpr int kMaxCols = 1 << 20;    // 256 rows of an operand lie within 2^31 bytes
-constexpr long long kMaxTiles = 1LL << 23;  // x 256 threads of a launch
+constexpr int kMaxRows = 1 << 21;
+constexpr int kMaxCols = 1 << 20;           // 256 rows of an operand lie within 2^31 bytes
+constexpr long long kMaxTiles = 1LL << 22;  // times 512 threads, a launch stays below 2^32
 
 struct Span {
   const void* p;

@@ -12,8 +12,10 @@ the library's PQ forward (bias and ReLU fused) and max-pool.
 
 The original network belongs to the caller: for every PQ layer it supplies
 the desired responses T, the original layer's linear response W * S_orig on
-the original network's own inputs (no bias, before the ReLU), as fp32.  Every
-step here is a library call; nothing is computed in torch.
+the original network's own inputs (no bias, before the ReLU), as fp32; for a
+stack of fully-connected layers `fc_responses` makes them with the library's
+dense layer (`qcnn_linear_forward`).  Every step here is a library call;
+nothing is computed in torch.
 """
 from __future__ import annotations
 
@@ -22,6 +24,27 @@ from typing import List, Optional
 import torch
 
 from . import api
+
+
+def fc_responses(x: torch.Tensor, specs: List[dict]) -> List[torch.Tensor]:
+    """The original network's responses T for a stack of fully-connected
+    layers: per spec (as for `quantize_network`, all "fc"), W * S_orig as fp32
+    [N][C_t], where the next layer's input is the response with bias and
+    ReLU.  x: the calibration batch, fp32, flattened to [N][C_s]."""
+    if any(spec["kind"] != "fc" for spec in specs):
+        raise ValueError("fc_responses takes fully-connected layers only")
+    h = x.reshape(x.shape[0], -1).contiguous()
+    out: List[torch.Tensor] = []
+    for spec in specs:
+        W, bias, act = spec["W"], spec.get("bias"), "relu" if spec["relu"] else "none"
+        if bias is None:  # the response is what the activation sees
+            T = torch.empty((h.shape[0], W.shape[0]), dtype=torch.float32, device=h.device)
+            h = api.linear_forward(h, W, act=act, pre=T)
+        else:
+            T = api.linear_forward(h, W)
+            h = api.linear_forward(h, W, bias, act=act)
+        out.append(T)
+    return out
 
 
 def quantize_network(x: torch.Tensor, specs: List[dict], targets: List[Optional[torch.Tensor]], sweeps: int = 1,
