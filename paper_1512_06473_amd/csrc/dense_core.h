@@ -199,52 +199,78 @@ __device__ __forceinline__ void store_quad(T* p, f4 v, int n) {
   }
 }
 
+// The bias of columns p .. p + 3 (zeros without one, and past the end).
 template <typename T>
-__device__ __forceinline__ void emit_linear(const Epi& e, int np, int q, int p, f4 v) {
+__device__ __forceinline__ f4 bias_quad(const Epi& e, int np, int p, int from = 0) {
+  if (!e.bias || p >= np) return f4{0.f, 0.f, 0.f, 0.f};
+  return load_quad(static_cast<const T*>(e.bias) + from + p, np - p);
+}
+
+// What becomes of U quads of columns p .. p + 3 in rows q, q + dq, ...: all
+// their loads first, so that they are on their way together.
+template <typename T, int U>
+__device__ __forceinline__ void emit_linear(const Epi& e, int np, int nq, int q, int dq, int p, f4 (&v)[U], f4 bias) {
   const int n = np - p;
   if (n <= 0) return;
-  if (e.acc_in) v += *reinterpret_cast<const f4*>(e.acc + q * e.ldacc + p);
+  if (e.acc_in) {
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (q + k * dq < nq) v[k] += *reinterpret_cast<const f4*>(e.acc + (q + k * dq) * e.ldacc + p);
+  }
   if (e.acc_out) {
-    *reinterpret_cast<f4*>(e.acc + q * e.ldacc + p) = v;
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (q + k * dq < nq) *reinterpret_cast<f4*>(e.acc + (q + k * dq) * e.ldacc + p) = v[k];
     return;
   }
-  if (e.alpha) v *= *e.alpha;
-  if (e.bias) v += load_quad(static_cast<const T*>(e.bias) + p, n);
-  if (e.pre) store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, v, n);
-  if (e.act != QCNN_ACT_NONE) {
+  f4 r[U];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act_value<T>(e.act, v[i]);
+  for (int k = 0; k < U; ++k) {
+    r[k] = f4{0.f, 0.f, 0.f, 0.f};
+    if (e.res && q + k * dq < nq) r[k] = load_quad(static_cast<const T*>(e.res) + (q + k * dq) * e.ldr + p, n);
   }
-  if (e.res) v += load_quad(static_cast<const T*>(e.res) + q * e.ldr + p, n);
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, v, n);
+  const float alpha = e.alpha ? *e.alpha : 1.f;
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    if (q + k * dq >= nq) break;
+    f4 z = v[k] * alpha + bias;
+    if (e.pre) store_quad(static_cast<T*>(e.pre) + (q + k * dq) * e.ldpre + p, z, n);
+    if (e.act != QCNN_ACT_NONE) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] = act_value<T>(e.act, z[i]);
+    }
+    if (e.res) z += r[k];
+    store_quad(static_cast<T*>(e.y) + (q + k * dq) * e.ldy + p, z, n);
+  }
 }
 
 // np: columns of the result (half of the weight's rows).
-template <typename T>
-__device__ __forceinline__ void emit_gated(const Epi& e, int np, int q, int p, f4 g, f4 u) {
+template <typename T, int U>
+__device__ __forceinline__ void emit_gated(const Epi& e, int np, int nq, int q, int dq, int p, f4 (&g)[U], f4 (&u)[U],
+                                           f4 bias_g, f4 bias_u) {
   const int n = np - p;
   if (n <= 0) return;
-  if (e.bias) {
-    g += load_quad(static_cast<const T*>(e.bias) + p, n);
-    u += load_quad(static_cast<const T*>(e.bias) + np + p, n);
-  }
-  if (e.pre) {
-    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + p, g, n);
-    store_quad(static_cast<T*>(e.pre) + q * e.ldpre + np + p, u, n);
-  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) g[i] = act_value<T>(e.act, g[i]) * u[i];
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, g, n);
+  for (int k = 0; k < U; ++k) {
+    if (q + k * dq >= nq) break;
+    f4 z = g[k] + bias_g, w = u[k] + bias_u;
+    if (e.pre) {
+      T* pre = static_cast<T*>(e.pre) + (q + k * dq) * e.ldpre + p;
+      store_quad(pre, z, n);
+      store_quad(pre + np, w, n);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = act_value<T>(e.act, z[i]) * w[i];
+    store_quad(static_cast<T*>(e.y) + (q + k * dq) * e.ldy + p, z, n);
+  }
 }
 
 // Logits with their bias; classes past the end become -inf.
-template <typename T>
-__device__ __forceinline__ f4 class_logits(const Epi& e, int np, int p, f4 v) {
-  const int n = np - p;
-  if (e.bias && n > 0) v += load_quad(static_cast<const T*>(e.bias) + e.class0 + p, n);
+__device__ __forceinline__ f4 class_logits(int np, int p, f4 v, f4 bias) {
+  v += bias;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i >= n) v[i] = -INFINITY;
+    if (i >= np - p) v[i] = -INFINITY;
   return v;
 }
 
@@ -253,23 +279,31 @@ __device__ __forceinline__ f4 class_logits(const Epi& e, int np, int p, f4 v) {
 // type's range nor rounds every label's entry the same way; times `gain`, a
 // power of two that keeps fp16's small probabilities off its subnormals.
 // y's rows are whole quads: what lies past np is written as 0.
-template <typename T>
-__device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int q, int p, f4 z) {
-  const long long label = e.labels[q];
-  z = class_logits<T>(e, np, p, z);
-  f4 d = {0.f, 0.f, 0.f, 0.f};
-  if (label >= 0) {
-    const float w = e.dloss[q] / *e.dmax * e.gain, lse = e.lse[q];
-    const long long at = label - e.class0;
+template <typename T, int U>
+__device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int nq, int q, int dq, int p, f4 (&z)[U], f4 bias) {
+  long long label[U];
+  float lse[U], w[U];
+  const float scale = e.gain / *e.dmax;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (p + i < np) d[i] = w * (Num<T>::exp_(z[i] - lse) - (at == p + i ? 1.f : 0.f));
-    if (label >= e.classes) d = f4{NAN, NAN, NAN, NAN};
+  for (int k = 0; k < U; ++k) {
+    const int row = min(q + k * dq, nq - 1);
+    label[k] = e.labels[row];
+    lse[k] = e.lse[row];
+    w[k] = e.dloss[row] * scale;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (p + i >= np) d[i] = 0.f;
-  store_quad(static_cast<T*>(e.y) + q * e.ldy + p, d, 4);
+  for (int k = 0; k < U; ++k) {
+    if (q + k * dq >= nq) break;
+    const f4 l = z[k] + bias;
+    const long long at = label[k] - e.class0;
+    f4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (p + i >= np || label[k] < 0) continue;
+      d[i] = label[k] >= e.classes ? NAN : w[k] * (Num<T>::exp_(l[i] - lse[k]) - (at == p + i ? 1.f : 0.f));
+    }
+    store_quad(static_cast<T*>(e.y) + (q + k * dq) * e.ldy + p, d, 4);
+  }
 }
 
 // (max, sum of exp(. - max)) of two disjoint sets.
@@ -502,6 +536,9 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
   if constexpr (EPI == kStats) {
     const int q_first = cq + wq * WQ + c;
     const int p_first = cp + wp * WP + 4 * g;
+    f4 bias[FP];
+#pragma unroll
+    for (int i = 0; i < FP; ++i) bias[i] = bias_quad<T>(e, a.np, p_first + 16 * i, e.class0);
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
       const int q = q_first + 16 * j;
@@ -510,7 +547,7 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
 #pragma unroll
       for (int i = 0; i < FP; ++i) {
         const int p = p_first + 16 * i;
-        const f4 z = class_logits<T>(e, a.np, p, acc[i][j]);
+        const f4 z = class_logits(a.np, p, acc[i][j], bias[i]);
         acc[i][j] = z;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
@@ -536,35 +573,44 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
     constexpr int kRows = kRoomBytes / (WP * 4) < WQ ? kRoomBytes / (WP * 4) : WQ;
     constexpr int kQuads = WP / 4, kOut = GATED ? kQuads / 2 : kQuads;  // of a row; that one emit covers
     static_assert(kQuads >= 16 && kRows % 16 == 0, "the XOR stays within a row");
+    const int quad = lane % kOut, p = cp + wp * (GATED ? WP / 2 : WP) + 4 * quad;  // a lane keeps its columns
+    f4 bias = {0.f, 0.f, 0.f, 0.f}, bias_up = bias;
+    if constexpr (EPI != kPartial) {
+      bias = bias_quad<T>(e, a.np, p, EPI == kXgrad ? e.class0 : 0);
+      if (GATED) bias_up = bias_quad<T>(e, a.np, p, a.np);
+    }
 #pragma unroll
     for (int first = 0; first < WQ; first += kRows) {
 #pragma unroll
       for (int j = 0; j < kRows / 16; ++j)
 #pragma unroll
         for (int i = 0; i < FP; ++i) room[(16 * j + c) * kQuads + ((4 * i + g) ^ c)] = acc[i][first / 16 + j];
-#pragma unroll 4
-      for (int t = 0; t < kRows * kOut / 64; ++t) {
-        const int row = t * (64 / kOut) + lane / kOut, quad = lane % kOut;
-        const int q = cq + wq * WQ + first + row, p = cp + wp * (GATED ? WP / 2 : WP) + 4 * quad;
-        const f4 v = room[row * kQuads + (quad ^ (row & 15))];
-        if (q >= a.nq) continue;
-        if constexpr (GATED) {
-          const f4 u = room[row * kQuads + ((quad + kOut) ^ (row & 15))];
-          if constexpr (EPI == kPartial) {
-            if (p < a.np) {
-              float* o = a.part + ((long long)split * a.nq + q) * a.ldpart + p;
-              *reinterpret_cast<f4*>(o) = v;
-              *reinterpret_cast<f4*>(o + a.ldpart / 2) = u;
-            }
-          } else {
-            emit_gated<T>(e, a.np, q, p, v, u);
+      constexpr int kAll = kRows * kOut / 64, U = kAll < 4 ? kAll : 4, kStep = 64 / kOut;
+#pragma unroll 1
+      for (int t = 0; t < kAll; t += U) {
+        const int row = t * kStep + lane / kOut, q = cq + wq * WQ + first + row;
+        f4 v[U], u[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int r = row + k * kStep;
+          v[k] = room[r * kQuads + (quad ^ (r & 15))];
+          u[k] = GATED ? room[r * kQuads + ((quad + kOut) ^ (r & 15))] : v[k];
+        }
+        if constexpr (EPI == kPartial) {
+          if (p >= a.np) continue;
+          float* o = a.part + ((long long)split * a.nq + q) * a.ldpart + p;
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            if (q + k * kStep >= a.nq) break;
+            *reinterpret_cast<f4*>(o + k * kStep * a.ldpart) = v[k];
+            if (GATED) *reinterpret_cast<f4*>(o + k * kStep * a.ldpart + a.ldpart / 2) = u[k];
           }
-        } else if constexpr (EPI == kPartial) {
-          if (p < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + p) = v;
+        } else if constexpr (GATED) {
+          emit_gated<T, U>(e, a.np, a.nq, q, kStep, p, v, u, bias, bias_up);
         } else if constexpr (EPI == kXgrad) {
-          if (p < e.ldy) emit_xgrad<T>(e, a.np, q, p, v);
+          if (p < e.ldy) emit_xgrad<T, U>(e, a.np, a.nq, q, kStep, p, v, bias);
         } else {
-          emit_linear<T>(e, a.np, q, p, v);
+          emit_linear<T, U>(e, a.np, a.nq, q, kStep, p, v, bias);
         }
       }
     }

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(const Few a, const 
       float2 t = make_float2(-INFINITY, 0.f);
 #pragma unroll
       for (int f = 0; f < FP; ++f) {
-        const f4 z = class_logits<T>(e, a.np, p + 16 * f, acc[f][j]);
+        const f4 z = class_logits(a.np, p + 16 * f, acc[f][j], bias_quad<T>(e, a.np, p + 16 * f, e.class0));
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           if (label == p + 16 * f + n && p + 16 * f + n < a.np) e.zlabel[q] = z[n];
@@ -161,7 +161,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(const Few a, const 
               *reinterpret_cast<f4*>(o + a.ldpart / 2) = acc[f + FP / 2][j];
             }
           } else {
-            emit_gated<T>(e, a.np, q, pf, acc[f][j], acc[f + FP / 2][j]);
+            f4 v[1] = {acc[f][j]}, u[1] = {acc[f + FP / 2][j]};
+            emit_gated<T, 1>(e, a.np, a.nq, q, 1, pf, v, u, bias_quad<T>(e, a.np, pf), bias_quad<T>(e, a.np, pf, a.np));
           }
         }
       } else {
@@ -171,9 +172,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(const Few a, const 
           if constexpr (EPI == kPartial) {
             if (pf < a.np) *reinterpret_cast<f4*>(a.part + ((long long)split * a.nq + q) * a.ldpart + pf) = acc[f][j];
           } else if constexpr (EPI == kXgrad) {
-            if (pf < e.ldy) emit_xgrad<T>(e, a.np, q, pf, acc[f][j]);
+            f4 v[1] = {acc[f][j]};
+            if (pf < e.ldy) emit_xgrad<T, 1>(e, a.np, a.nq, q, 1, pf, v, bias_quad<T>(e, a.np, pf, e.class0));
           } else {
-            emit_linear<T>(e, a.np, q, pf, acc[f][j]);
+            f4 v[1] = {acc[f][j]};
+            emit_linear<T, 1>(e, a.np, a.nq, q, 1, pf, v, bias_quad<T>(e, a.np, pf));
           }
         }
       }

@@ -229,9 +229,11 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ p
     }
   }
   if (q >= nq) return;
-  if constexpr (EPI == kGated) emit_gated<T>(e, np, q, p, v, u);
-  else if constexpr (EPI == kXgrad) emit_xgrad<T>(e, np, q, p, v);
-  else emit_linear<T>(e, np, q, p, v);
+  f4 v1[1] = {v}, u1[1] = {u};
+  const f4 bias = bias_quad<T>(e, np, p, EPI == kXgrad ? e.class0 : 0);
+  if constexpr (EPI == kGated) emit_gated<T, 1>(e, np, nq, q, 1, p, v1, u1, bias, bias_quad<T>(e, np, p, np));
+  else if constexpr (EPI == kXgrad) emit_xgrad<T, 1>(e, np, nq, q, 1, p, v1, bias);
+  else emit_linear<T, 1>(e, np, nq, q, 1, p, v1, bias);
 }
 
 __device__ __forceinline__ void write_loss(float2 t, float zlabel, long long label, int classes, float* loss,
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(256) void finish_loss_kernel(const float* __restric
     f4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int i = 0; i < splits; ++i) z += *reinterpret_cast<const f4*>(part + i * each + q * ldpart + p);
-    z = class_logits<T>(e, np, p, z);
+    z = class_logits(np, p, z, bias_quad<T>(e, np, p, e.class0));
     const float m = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
     float sum = 0.f;
 #pragma unroll
