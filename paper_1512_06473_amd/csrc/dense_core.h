@@ -20,9 +20,10 @@
 // MFMA's first operand is P: a lane ends up with 4 consecutive p of one q.
 //
 // Bounds: an operand is read through a buffer descriptor whose extent ends
-// with its last element, so rows past the end read as 0; the tail of k is
-// cut off lane by lane (C) or by the extent (S).  p and q past the end are
-// not stored.
+// with its last element, so rows past the end read as 0 (each of a load's four
+// dwords is checked by itself; rows need to start at whole dwords only); the
+// tail of k is cut off lane by lane (C; within 16 bytes, in LDS) or by the
+// extent (S).  p and q past the end are not stored.
 #pragma once
 
 #include <type_traits>
@@ -321,9 +322,9 @@ struct Prod {
   const char* p;
   const char* q;
   long long ldp, ldq;   // bytes
-  int np, nq, nk;       // outputs and terms; nk of a C operand in whole 16 bytes
+  int np, nq, nk;       // outputs and terms
   int kp, kq;           // rows that an S operand has (C: unused)
-  int colsp, colsq;     // columns that an S operand stores, whole 16 bytes
+  int colsp, colsq;     // columns that an S operand stores, whole dwords (as nk of a C operand)
   int p2;               // kGated: rows between a gate row and its up row
   int p0, p1, q0, q1;   // the outputs of this launch; kStats: their first slot
   int slot0;
@@ -509,6 +510,7 @@ __device__ __forceinline__ bool gated_up(int r) { return r % WP >= WP / 2; }
 // Where a workgroup's tile lies.
 struct Place {
   int tp, cp, cq, split, step0, nsteps;
+  bool ragged;  // its last step ends within 16 bytes of k
 };
 
 template <int BC, int BQ, int S>
@@ -519,8 +521,30 @@ __device__ __forceinline__ Place place_of(const Prod& a) {
   t.cp = a.p0 + t.tp * BC;
   t.cq = a.q0 + tq * BQ;
   t.step0 = t.split * a.steps;
-  t.nsteps = min(a.steps, (a.nk * S + 127) / 128 - t.step0);
+  const int all = (int)(((long long)a.nk * S + 127) / 128);
+  t.nsteps = min(a.steps, all - t.step0);
+  t.ragged = (a.nk * S & 15) && t.step0 + t.nsteps == all;
   return t;
+}
+
+// The lane's number, counted anew: no register holds it through the loop.
+__device__ __forceinline__ int fresh_lane() {
+  int ones = -1;
+  asm volatile("" : "+s"(ones));
+  return __builtin_amdgcn_mbcnt_hi(ones, __builtin_amdgcn_mbcnt_lo(ones, 0));
+}
+
+// In the tiles of a ragged last step, zeros from its `left` bytes of k on to
+// the next 16 (what lies behind the rows' ends was loaded there): a row per
+// thread.  Between a barrier that the tiles are complete behind and another.
+template <bool PS, bool QS, int BP, int BQ>
+__device__ __forceinline__ void zero_tail(char* lp, char* lq, int left, int wave) {
+  const int id = wave * 64 + fresh_lane();
+  const bool is_p = id < BP;
+  const int r = is_p ? id : id - BP;
+  if (is_p ? PS : QS || r >= BQ) return;
+  char* at = (is_p ? lp : lq) + r * 128 + (((left >> 4) ^ ((r >> 1) & 7)) << 4);
+  for (int d = left & 15; d < 16; d += 4) *reinterpret_cast<uint32_t*>(at + d) = 0;
 }
 
 constexpr int kRoomBytes = 16384;
@@ -639,6 +663,8 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   const int wp = wave % NWP, wq = wave / NWP;
   const Place t = place_of<GATED ? BP / 2 : BP, BQ, sizeof(T)>(a);
   const int nsteps = t.nsteps;
+  // Large tiles have no registers left for it: their rows end with 16 bytes.
+  const bool ragged = BP == 128 && (!PS || !QS) && t.ragged;
   const Walk<T, PS, BP, NW> walk_p(a.p, a.ldp, t.cp, a.np, a.colsp, a.nk, a.kp, wave, lane, true);
   const Walk<T, QS, BQ, NW> walk_q(a.q, a.ldq, t.cq, a.nq, a.colsq, a.nk, a.kq, wave, lane, true);
 
@@ -711,12 +737,16 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   // further on is sent for, and the next step's first half is read under the
   // second half's products.
   Frags f0, f1;
-  auto body = [&](int s, char* lp, char* lq, const char* next_p, const char* next_q) __attribute__((always_inline)) {
+  auto body = [&](int s, char* lp, char* lq, char* next_p, char* next_q) __attribute__((always_inline)) {
     read(f1, lp, lq, 1);
     multiply(f0);
     interleave(std::integral_constant<int, 0>());
     __builtin_amdgcn_sched_barrier(0);
     wait_and_meet<(DEPTH - 2) * kFlight>();
+    if (ragged && s + 2 == nsteps) {
+      zero_tail<PS, QS, BP, BQ>(next_p, next_q, walk_p.left(t.step0 + s + 1), wave);
+      meet();
+    }
     stage(s + DEPTH, lp, lq);
     read(f0, next_p, next_q, 0);
     multiply(f1);
@@ -727,6 +757,10 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
 #pragma unroll
   for (int b = 0; b < DEPTH; ++b) stage(b, ps[b], qs[b]);
   wait_and_meet<(DEPTH - 1) * kFlight>();
+  if (ragged && nsteps == 1) {
+    zero_tail<PS, QS, BP, BQ>(p0, q0, walk_p.left(t.step0), wave);
+    meet();
+  }
   read(f0, p0, q0, 0);
   int s = 0;
   for (; s + DEPTH <= nsteps; s += DEPTH) {
@@ -744,8 +778,8 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
 #pragma unroll
   for (int b = 1; b < 4; ++b)
     if (wave / kPer == b) room = b == 1 ? p1 : b == 2 ? q0 : q1;
-  finish_tile<T, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, reinterpret_cast<f4*>(room + wave % kPer * kRoomBytes), lane,
-                                          wp, wq);
+  finish_tile<T, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, reinterpret_cast<f4*>(room + wave % kPer * kRoomBytes),
+                                          fresh_lane(), wp, wq);
 #endif
 }
 
@@ -833,8 +867,14 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
       ahead[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(descriptor(walk_q, step, none), v, 0, 0));
     }
   };
-  auto put = [&](char* buffer, int j) __attribute__((always_inline)) {
+  auto put = [&](char* buffer, int s, int j) __attribute__((always_inline)) {
     const bool is_p = j < LP::kLoads;
+    if ((is_p ? !PS : !QS) && t.ragged && s + 1 == t.nsteps) {  // what lies behind a row's end
+      const int left = walk_p.left(t.step0 + s), chunk = is_p ? walk_p.chunk : walk_q.chunk;
+#pragma unroll
+      for (int i = 1; i < 4; ++i)
+        if (chunk + 4 * i >= left) ahead[j][i] = 0.f;
+    }
     char* o = is_p ? buffer + LP::write_at(write_p, j) : buffer + LP::kBytes + LQ::write_at(write_q, j - LP::kLoads);
     uint2 w[3];
     split_bf16(ahead[j], w);
@@ -846,7 +886,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
   for (int j = 0; j < kLoads; ++j) load(0, j);
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
-    put(lds, j);
+    put(lds, 0, j);
     load(1, j);
   }
   meet();
@@ -866,7 +906,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < kFirst; ++j) {
-      put(next, j);
+      put(next, s + 1, j);
       load(s + 2, j);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -885,7 +925,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
       }
 #pragma unroll
       for (int j = kFirst + i * (kLoads - kFirst) / FP; j < kFirst + (i + 1) * (kLoads - kFirst) / FP; ++j) {
-        put(next, j);
+        put(next, s + 1, j);
         load(s + 2, j);
       }
     }
@@ -926,6 +966,10 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
             descriptor(again_q, step, false), (lds_void*)(lds + OP::kBytes + (wave + j * NW) * 1024), 16,
             again_q.offset(OQ::first(wave, j), OQ::chunk_delta(j), left), 0, 0, 0);
       wait_and_meet<0>();
+      if (t.ragged && s + 1 == t.nsteps) {
+        zero_tail<PS, QS, BP, BQ>(lds, lds + OP::kBytes, left, wave);
+        meet();
+      }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll

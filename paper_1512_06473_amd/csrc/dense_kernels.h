@@ -26,10 +26,11 @@ constexpr int pad16(int n) {  // elements, to whole 16 bytes
   return (n + u - 1) / u * u;
 }
 
+// Rows that the products read where they are: they start at whole dwords
+// (always, in fp32).
 template <typename T>
-bool wide(const void* p, long long ld, int cols) {  // rows of whole aligned 16 bytes
-  constexpr int u = 16 / (int)sizeof(T);
-  return ((uintptr_t)p & 15) == 0 && ld % u == 0 && cols % u == 0;
+bool direct(const void* p, long long ld, int cols) {
+  return ((uintptr_t)p & 3) == 0 && ld * sizeof(T) % 4 == 0 && cols * sizeof(T) % 4 == 0;
 }
 
 // ------------------------------------------------------ kernels around them
@@ -65,6 +66,8 @@ struct Slope {
   const void* pre;
   void* dz;     // null: only the sums
   float* part;  // null: no sums
+  void* sums;   // T: the finished sums, where one block row has all rows
+  const float* alpha;
   long long lddy, ldpre, lddz;
   int rows, cols, chunk, act;  // cols: of dy
 };
@@ -150,7 +153,15 @@ __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
       for (int k = 0; k < kQ; ++k) s0[k] += dy[k];
     }
   }
-  if (a.part) {
+  if (a.sums) {
+    T* o = static_cast<T*>(a.sums) + p;
+    const float alpha = a.alpha ? *a.alpha : 1.f;
+#pragma unroll
+    for (int k = 0; k < kQ; ++k) {
+      store_quad(o + 4 * k, s0[k] * alpha, n - 4 * k);
+      if (GATED) store_quad(o + a.cols + 4 * k, s1[k] * alpha, n - 4 * k);
+    }
+  } else if (a.part) {
     float* o = a.part + blockIdx.y * width + p;
 #pragma unroll
     for (int k = 0; k < kQ; ++k) {
@@ -179,17 +190,22 @@ __global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ p
   out[c] = (T)(alpha ? s * *alpha : s);
 }
 
-// Rows of a thread: enough blocks for the chip, at most 512 rows of sums.
-inline int slope_chunk(int rows) { return std::max(4, ceil_div(rows, 512)); }
+// Rows of a thread: all of a few, which saves the kernel that joins the sums;
+// else enough blocks for the chip, and at most 512 rows of sums.
+inline int slope_chunk(int rows) { return rows <= 16 ? rows : std::max(4, ceil_div(rows, 512)); }
 
 // dz and, with dbias, alpha times its sums over rows.
 template <typename T, bool GATED>
-hipError_t run_slope(const Slope& a, void* dbias, const float* alpha, hipStream_t st) {
+hipError_t run_slope(Slope a, void* dbias, const float* alpha, hipStream_t st) {
   const int chunks = ceil_div(a.rows, a.chunk), width = GATED ? 2 * a.cols : a.cols;
   const int threads = ceil_div(a.cols, 16 / (int)sizeof(T)) + 1;
+  if (chunks == 1) {
+    a.sums = dbias;
+    a.alpha = alpha;
+  }
   slope_kernel<T, GATED><<<dim3(ceil_div(threads, 256), chunks), 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !dbias) return e;
+  if (e != hipSuccess || !dbias || chunks == 1) return e;
   colsum_kernel<T><<<ceil_div(width, 64), 256, 0, st>>>(a.part, chunks, width, alpha, static_cast<T*>(dbias));
   return hipGetLastError();
 }
@@ -472,6 +488,10 @@ hipError_t run_product(Prod a, const Epi& e, const Cut& c, float* part, hipStrea
   return err != hipSuccess ? err : finish<T, EPI>(a.np, a.nq, e, c, part, st);
 }
 
+// Whether a product's operands along k have to end with whole 16 bytes.
+template <typename T>
+bool ends_whole(const Cut& c) { return sizeof(T) == 2 && c.big; }
+
 // Slots of a product that is not split: one per wave along p (the same for
 // every row, so none of its rows may go in tiles of another size).
 template <typename T>
@@ -523,6 +543,7 @@ struct Forward : Cut {
   }
 
   int cols() const { return wide_ ? 32 : 16; }  // result columns of a wave
+  bool whole() const { return !few && ends_whole<T>(*this); }
 
   template <int EPI, bool GATED>
   hipError_t launch_few(const Few& a, const Epi& e, hipStream_t st) const {
@@ -535,9 +556,10 @@ struct Forward : Cut {
     return timed_launch(&timer, few_kernel<T, 2, 1, EPI, GATED>, grid, block, 0u, st, a, e);
   }
 
-  // w and x: rows of ldw and ldx bytes; as the tiles read them unless `few`.
+  // w and x: rows of ldw and ldx bytes; as the tiles read them unless `few`,
+  // with `stored` columns in both.
   template <int EPI, bool GATED>
-  hipError_t run(const char* w, long long ldw, const char* x, long long ldx, const Epi& e, float* part,
+  hipError_t run(const char* w, long long ldw, const char* x, long long ldx, int stored, const Epi& e, float* part,
                  hipStream_t st) const {
     if (!few) {
       Prod a = {};
@@ -547,7 +569,7 @@ struct Forward : Cut {
       a.ldq = ldx;
       a.np = a.p2 = np;
       a.nq = nq;
-      a.nk = pad16<T>(nk);
+      a.nk = stored;
       return run_product<T, false, false, EPI, GATED>(a, e, *this, part, st);
     }
     Few a = {w, x, ldw, ldx, np, nq, nk, np, ks, steps, splits, part, ldpart};
@@ -565,8 +587,10 @@ struct Source {
   int rows, cols;
   bool copy;
   size_t at = 0;
-  Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l, bool tiles = true)
-      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(tiles && !wide<T>(ptr, ld_, cols_)) {
+  // tiles: the products read it; whole: and want the rows' ends, along k, to be
+  // those of 16 bytes.
+  Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l, bool tiles = true, bool whole = false)
+      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(tiles && (!direct<T>(ptr, ld_, cols_) || (whole && cols_ * sizeof(T) % 16)))  {
     if (copy) at = l->add((size_t)rows * pad16<T>(cols) * sizeof(T));
   }
   hipError_t place(char* ws, hipStream_t st) {
@@ -581,6 +605,7 @@ struct Source {
   }
   long long bytes() const { return ld * (long long)sizeof(T); }
   const char* ptr() const { return reinterpret_cast<const char*>(p); }
+  int stored() const { return copy ? pad16<T>(cols) : cols; }  // columns, whole dwords
 };
 
 // ------------------------------------------------------------------- calls
@@ -603,7 +628,7 @@ hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, co
                           const void* res, void* pre, void* y, const Room& room, hipStream_t st) {
   Layout l;
   const Forward<T> c(s.Ct, s.N, s.Cs, false);
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few, c.whole()), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few, c.whole());
   const size_t part = l.add(c.part_bytes);
   Scratch ws;
   bool asked;
@@ -621,7 +646,8 @@ hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, co
   p.res = res;
   p.ldr = s.ldr;
   p.act = act;
-  return c.template run<kLinear, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
+  return c.template run<kLinear, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
+                                     std::min(wsrc.stored(), xs.stored()), p,
                                                       reinterpret_cast<float*>(ws.get() + part), st);
 }
 
@@ -630,7 +656,7 @@ hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, con
                          void* y, const Room& room, hipStream_t st) {
   Layout l;
   const Forward<T> c(s.Ct, s.N, s.Cs, true);
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, 2 * s.Ct, s.Cs, &l, !c.few);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few, c.whole()), wsrc(w, s.Cs, 2 * s.Ct, s.Cs, &l, !c.few, c.whole());
   const size_t part = l.add(c.part_bytes);
   Scratch ws;
   bool asked;
@@ -646,39 +672,41 @@ hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, con
   p.ldpre = 2LL * s.Ct;
   p.bias = bias;
   p.act = act;
-  return c.template run<kGated, true>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
+  return c.template run<kGated, true>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
+                                     std::min(wsrc.stored(), xs.stored()), p,
                                                     reinterpret_cast<float*>(ws.get() + part), st);
 }
 
 // dx = dz w, as fp32 running sums in `acc` or finished in y.
+// stored: dz's columns, whole dwords (zeros past the weight's rows).
 template <typename T>
-Prod dx_prod(const Source<T>& w, const char* wp, int wrows, const char* dz, long long lddz, int N) {
+Prod dx_prod(const Source<T>& w, const char* wp, int wrows, const char* dz, long long lddz, int stored, int N) {
   Prod a = {};
   a.p = wp;
   a.ldp = w.bytes();
   a.np = w.cols;
-  a.colsp = pad16<T>(w.cols);
+  a.colsp = w.stored();
   a.kp = wrows;
   a.q = dz;
   a.ldq = lddz * (long long)sizeof(T);
   a.nq = N;
-  a.nk = pad16<T>(wrows);
+  a.nk = stored;
   return a;
 }
 
 // dw = dz^T x
 template <typename T>
-Prod dw_prod(const Source<T>& x, const char* dz, long long lddz, int wrows) {
+Prod dw_prod(const Source<T>& x, const char* dz, long long lddz, int stored, int wrows) {
   Prod a = {};
   a.p = x.ptr();
   a.ldp = x.bytes();
   a.np = x.cols;
-  a.colsp = pad16<T>(x.cols);
+  a.colsp = x.stored();
   a.kp = x.rows;
   a.q = dz;
   a.ldq = lddz * (long long)sizeof(T);
   a.nq = wrows;
-  a.colsq = pad16<T>(wrows);
+  a.colsq = stored;
   a.kq = x.rows;
   a.nk = x.rows;
   return a;
@@ -691,13 +719,15 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
   const int rows = GATED ? 2 * s.Ct : s.Ct;
   Layout l;
   // With no activation dy is dz, where the products can read it in place.
-  const bool in_place = !GATED && act == QCNN_ACT_NONE && (wide<T>(dy, s.ldy, s.Ct) || (!dx && !dw));
+  const Cut cx = cut_of<T>(s.Cs, s.N, pad16<T>(rows), false), cw = cut_of<T>(s.Cs, rows, s.N, false);
+  const bool fits = direct<T>(dy, s.ldy, s.Ct) && !(dx && ends_whole<T>(cx) && s.Ct * sizeof(T) % 16);
+  const bool in_place = !GATED && act == QCNN_ACT_NONE && (fits || (!dx && !dw));
   const long long lddz = in_place ? s.ldy : pad16<T>(rows);
+  const int stored = in_place ? rows : pad16<T>(rows);
   const size_t dz_at = in_place ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
   const int chunk = slope_chunk(s.N), chunks = ceil_div(s.N, chunk);
   const size_t sums_at = dbias ? l.add((size_t)chunks * rows * 4) : 0;
   Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
-  const Cut cx = cut_of<T>(s.Cs, s.N, pad16<T>(rows), false), cw = cut_of<T>(s.Cs, rows, s.N, false);
   const size_t part = l.add(std::max(dx ? cx.part_bytes : 0, dw ? cw.part_bytes : 0));
   Scratch ws;
   bool asked;
@@ -728,14 +758,14 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Epi p = {};
     p.y = dx;
     p.ldy = s.Cs;
-    e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr(), rows, dz, lddz, s.N), p, cx, sums, st);
+    e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr(), rows, dz, lddz, stored, s.N), p, cx, sums, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
     Epi p = {};
     p.y = dw;
     p.ldy = s.Cs;
-    e = run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, rows), p, cw, sums, st);
+    e = run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, stored, rows), p, cw, sums, st);
   }
   return e;
 }
@@ -745,7 +775,7 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
                         float* loss, float* lse, const Room& room, hipStream_t st) {
   Layout l;
   const Forward<T> c(s.Ct, s.N, s.Cs, false, true);
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !c.few, c.whole()), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !c.few, c.whole());
   const int slots = c.slots;
   const size_t part = l.add(c.part_bytes), stat = l.add((size_t)slots * s.N * 8), zl = l.add((size_t)s.N * 4);
   Scratch ws;
@@ -763,7 +793,8 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   p.classes = s.Ct;
   p.loss = loss;
   p.lse_out = lse;
-  e = c.template run<kStats, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(), p,
+  e = c.template run<kStats, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
+                                     std::min(wsrc.stored(), xs.stored()), p,
                                                   reinterpret_cast<float*>(ws.get() + part), st);
   if (e != hipSuccess || slots == 0) return e;
   // 16 rows read whole 128-byte lines; fewer than 64 rows would leave most of
@@ -783,11 +814,16 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
                          const float* lse, const float* dloss, void* dx, void* dw, void* dbias, const Room& room,
                          hipStream_t st) {
   Layout l;
-  const bool few = s.N <= kFewRows<T>;
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, !few || dw), wsrc(w, s.Cs, s.Ct, s.Cs, &l, !few || dx);
   long long fit = (long long)(kPieceBytes / ((size_t)s.N * sizeof(T))) / 256 * 256;
   if (fit < 256) fit = 256;
   const int piece = fit < s.Ct ? (int)fit : s.Ct, pieces = ceil_div(s.Ct, piece);
+  bool tiles = false, whole = false;
+  for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
+    const Forward<T> f(n, s.N, s.Cs, false);
+    tiles |= !f.few;
+    whole |= f.whole();
+  }
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, tiles || dw, whole), wsrc(w, s.Cs, s.Ct, s.Cs, &l, tiles || dx, whole);
   const long long ldd = pad16<T>(piece), ldacc = (s.Cs + 3) / 4 * 4;
   const size_t d_at = l.add((size_t)s.N * ldd * sizeof(T)), scale_at = l.add(8);
   const size_t acc_at = dx && pieces > 1 ? l.add((size_t)s.N * ldacc * 4) : 0;
@@ -828,7 +864,8 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
     p.class0 = c0;
     p.classes = s.Ct;
     e = Forward<T>(n, s.N, s.Cs, false).template run<kXgrad, false>(wsrc.ptr() + c0 * wsrc.bytes(), wsrc.bytes(),
-                                                                    xs.ptr(), xs.bytes(), p, sums, st);
+                                                                    xs.ptr(), xs.bytes(),
+                                                                    std::min(wsrc.stored(), xs.stored()), p, sums, st);
     if (e == hipSuccess && dbias) {
       Slope b = {};
       b.dy = d;
@@ -849,7 +886,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       o.ldacc = ldacc;
       o.acc_in = k > 0;
       o.acc_out = k + 1 < pieces;
-      e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr() + c0 * wsrc.bytes(), n, d, ld, s.N), o,
+      e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr() + c0 * wsrc.bytes(), n, d, ld, (int)ld, s.N), o,
                                                       cut_of<T>(s.Cs, s.N, pad16<T>(n), false), sums, st);
     }
     if (e == hipSuccess && dw) {
@@ -857,7 +894,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       o.y = static_cast<T*>(dw) + (long long)c0 * s.Cs;
       o.ldy = s.Cs;
       o.alpha = scale + 1;
-      e = run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, n), o, cut_of<T>(s.Cs, n, s.N, false), sums,
+      e = run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, (int)ld, n), o, cut_of<T>(s.Cs, n, s.N, false), sums,
                                                      st);
     }
   }

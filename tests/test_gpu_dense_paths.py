@@ -415,3 +415,38 @@ def test_responses_of_a_stack_and_its_quantization(dev):
     assert all(float(q["objective"][-1]) <= float(q["objective"][0]) * (1 + 1e-9) for q in got)
     with pytest.raises(ValueError):
         quantize_net.fc_responses(x.to(dev), [{"kind": "pool", "k": 3, "s": 2}])
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Cs,Ct", [(40, 2, 6), (40, 66, 30), (300, 1002, 130), (129, 4094, 258), (1030, 1006, 1030),
+                                     (4096, 70, 4098)])
+def test_rows_that_end_within_16_bytes(dev, tname, N, Cs, Ct):
+    """Rows of whole dwords are read in place; what lies behind their ends (NaN
+    here, in x, dy and behind the last row) is not."""
+    T = TYPES[tname]
+    wide_x = torch.full((N, Cs + 2), float("nan"), dtype=T, device=dev)
+    wide_dy = torch.full((N, Ct + 2), float("nan"), dtype=T, device=dev)
+    flat_w = torch.full((Ct * Cs + 64,), float("nan"), dtype=T, device=dev)
+    x, dy, w = wide_x[:, :Cs], wide_dy[:, :Ct], flat_w[:Ct * Cs].view(Ct, Cs)
+    x.copy_(normal(dev, T, 1, N, Cs))
+    dy.copy_(normal(dev, T, 2, N, Ct))
+    w.copy_(normal(dev, T, 3, Ct, Cs))
+    xd, wd, dyd = x.double(), w.double(), dy.double()
+    print("row ends", tname, N, Cs, Ct, flush=True)
+    y = torch.mm(xd, wd.t())
+    near(api.linear_forward(x, w), y, product_bound(Cs, torch.mm(xd.abs(), wd.abs().t()), y, T), "y")
+    dx, dw, db = api.linear_backward(dy, x, w)
+    for got, ref, A, n, what in ((dx, torch.mm(dyd, wd), torch.mm(dyd.abs(), wd.abs()), Ct, "dx"),
+                                 (dw, torch.mm(dyd.t(), xd), torch.mm(dyd.abs().t(), xd.abs()), N, "dw"),
+                                 (db, dyd.sum(0), dyd.abs().sum(0), N, "dbias")):
+        near(got, ref, product_bound(n, A, ref, T), what)
+    g = api.gated_forward(x, w, act="relu")
+    assert torch.isfinite(g).all()
+    labels = torch.arange(N, device=dev) % Ct
+    loss, _ = api.linear_xent_forward(x, w, labels)
+    assert torch.allclose(loss.double(), torch.logsumexp(y, 1) - y.gather(1, labels[:, None])[:, 0], rtol=1e-4, atol=1e-3)
+    # an infinity: fp32's second way, over the same row ends
+    x[1, Cs - 1] = float("inf")
+    got = api.linear_forward(x, w)
+    assert torch.equal(got[1], torch.copysign(torch.full_like(got[1], float("inf")), w[:, Cs - 1]))
+    assert torch.isfinite(got[2:]).all()
