@@ -365,24 +365,29 @@ struct Edge {
   }
 };
 
-// The cut that should take the least time: the steps in a row of the busiest
-// CU, times what one takes.  A CU holds one tile, or two small 16-bit ones,
-// which hide each other's waits.  Measured per step on whole products (k of
-// 4096, 64 to 1024 tiles), in 16-bit types: a small tile alone 0.6 to 0.75 us,
-// two 1.15, a large one 1.4 to 1.7 (four small ones' work); fp32 1.4, a large
-// one (twice the work) 2.4 to 2.65.  Parts of k are
-// written and read once in fp32 (5 TB/s) and take a second kernel.  Against
-// the best of all measured cuts of ten shapes the choice loses 0 to 12 %; one
-// fixed rule (256 workgroups) lost up to 1.4 times.
+// The cut that should take the least time: the rounds of tiles that the busiest
+// CU goes through, times what one takes: `step` for each step and `ends` for
+// its first loads and its epilogue.  A CU holds one tile, or two small 16-bit
+// ones, which hide each other's waits.  Measured in us on whole products (64 to
+// 1024 tiles, k from 64 to 4096), step and ends: 16-bit types, a small tile
+// alone 0.55 to 0.75 and 4, two 1.05 and 6, a large one (the work of four) 1.6
+// and 10; fp32, a small tile 1.4 and 6, a large one (of two) 2.35 and 9.  Parts
+// of k are written and read once in fp32 (5 TB/s) and take a second kernel.
+// Against the best of all measured cuts of ten shapes the choice loses 0 to 12
+// %; one fixed rule (256 workgroups) lost up to 1.4 times, and a model without
+// the ends 1.2 times where k is short (774 x 100 -> 104192: 107 us).
 // A last round of large tiles that would leave most CUs idle goes in small ones
 // (1999 rows to 50001 classes: 6.1 rounds).  rows_alike: not along q.
 template <typename T>
 Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
   constexpr bool f32 = sizeof(T) == 4;
-  const double one = f32 ? 1.4 : 0.66, two = 1.15, large = f32 ? 2.5 : 1.6;
   const int all = ceil_div(nk * (int)sizeof(T), 128);
-  auto small_rounds = [&](long long groups) {
-    if (f32) return (groups + 255) / 256 * one;
+  auto large_rounds = [&](long long groups, int steps) {
+    return (groups + 255) / 256 * (f32 ? 2.35 * steps + 9. : 1.6 * steps + 10.);
+  };
+  auto small_rounds = [&](long long groups, int steps) {
+    if (f32) return (groups + 255) / 256 * (1.4 * steps + 6.);
+    const double one = 0.62 * steps + 4., two = 1.05 * steps + 6.;
     const long long rest = groups % 512;
     return groups / 512 * two + (rest > 256 ? two : rest ? one : 0.);
   };
@@ -393,8 +398,8 @@ Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
     for (int n = 1; n <= 32 && (n == 1 || (n <= all / 2 && tiles * n <= 1024)); ++n) {
       const int steps = ceil_div(all, n), splits = ceil_div(all, steps);
       const long long groups = tiles * splits;
-      const double rounds = big ? (groups + 255) / 256 * large : small_rounds(groups);
-      const double t = steps * rounds + (splits > 1 ? 4. + 1.6e-6 * splits * nq * np * (gated ? 2 : 1) : 0.);
+      const double t = (big ? large_rounds(groups, steps) : small_rounds(groups, steps)) +
+                       (splits > 1 ? 4. + 1.6e-6 * splits * nq * np * (gated ? 2 : 1) : 0.);
       if (t >= least) continue;
       least = t;
       best.big = big;
@@ -410,7 +415,7 @@ Cut cut_of(int np, int nq, int nk, bool gated, bool rows_alike = false) {
     if (main < 1 || main >= mine) continue;
     const long long tail = axis ? Edge<T>::tiles(np, nq - main * high, gated, false)
                                 : Edge<T>::tiles(np - main * wide, nq, gated, false);
-    const double t = all * (((long long)main * other + 255) / 256 * large + small_rounds(tail)) + 4.;
+    const double t = large_rounds((long long)main * other, all) + small_rounds(tail, all) + 4.;
     if (t >= least) continue;
     least = t;
     best.big = best.splits = 1;
