@@ -282,26 +282,32 @@ __device__ __forceinline__ f4 class_logits(int np, int p, f4 v, f4 bias) {
 // y's rows are whole quads: what lies past np is written as 0.
 template <typename T, int U>
 __device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int nq, int q, int dq, int p, f4 (&z)[U], f4 bias) {
-  long long label[U];
+  int at[U];  // the label's place from p on
   float lse[U], w[U];
+  bool counted[U];
   const float scale = e.gain / *e.dmax;
 #pragma unroll
   for (int k = 0; k < U; ++k) {
     const int row = min(q + k * dq, nq - 1);
-    label[k] = e.labels[row];
+    const long long label = e.labels[row];
+    counted[k] = label >= 0;
+    at[k] = label >= e.classes ? -1 : (int)label - e.class0 - p;
     lse[k] = e.lse[row];
-    w[k] = e.dloss[row] * scale;
+    w[k] = label >= e.classes ? NAN : e.dloss[row] * scale;
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
     if (q + k * dq >= nq) break;
     const f4 l = z[k] + bias;
-    const long long at = label[k] - e.class0;
     f4 d = {0.f, 0.f, 0.f, 0.f};
+    if (counted[k]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (p + i >= np || label[k] < 0) continue;
-      d[i] = label[k] >= e.classes ? NAN : w[k] * (Num<T>::exp_(l[i] - lse[k]) - (at == p + i ? 1.f : 0.f));
+      for (int i = 0; i < 4; ++i) d[i] = w[k] * (Num<T>::exp_(l[i] - lse[k]) - (at[k] == i ? 1.f : 0.f));
+    }
+    if (np - p < 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= np - p) d[i] = 0.f;
     }
     store_quad(static_cast<T*>(e.y) + (q + k * dq) * e.ldy + p, d, 4);
   }
@@ -558,32 +564,39 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
   const int tp = at.tp, cp = at.cp, cq = at.cq, split = at.split;
   const int g = lane >> 4, c = lane & 15;
   if constexpr (EPI == kStats) {
-    const int q_first = cq + wq * WQ + c;
-    const int p_first = cp + wp * WP + 4 * g;
-    f4 bias[FP];
+    const int q_first = cq + wq * WQ + c, p_wave = cp + wp * WP, p_first = p_wave + 4 * g;
+    if (e.bias || p_wave + WP > a.np) {  // else the sums are the logits
 #pragma unroll
-    for (int i = 0; i < FP; ++i) bias[i] = bias_quad<T>(e, a.np, p_first + 16 * i, e.class0);
+      for (int i = 0; i < FP; ++i) {
+        const f4 bias = bias_quad<T>(e, a.np, p_first + 16 * i, e.class0);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) acc[i][j] = class_logits(a.np, p_first + 16 * i, acc[i][j], bias);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
       const int q = q_first + 16 * j;
       const long long label = q < a.nq ? e.labels[q] - e.class0 : -1;
       float m = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < FP; ++i) {
-        const int p = p_first + 16 * i;
-        const f4 z = class_logits(a.np, p, acc[i][j], bias[i]);
-        acc[i][j] = z;
+      for (int i = 0; i < FP; ++i)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          m = fmaxf(m, z[n]);
-          if (label == p + n && p + n < a.np) e.zlabel[q] = z[n];
-        }
-      }
+        for (int n = 0; n < 4; ++n) m = fmaxf(m, acc[i][j][n]);
+      // The difference first: a mask of the type's lowest value must not overflow.
+      const float top = m == -INFINITY ? 0.f : m;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < FP; ++i)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) sum += acc[i][j][n] == -INFINITY ? 0.f : __expf(acc[i][j][n] - m);
+        for (int n = 0; n < 4; ++n) sum += __expf(acc[i][j][n] - top);
+      if (label >= p_wave && label < min(p_wave + WP, a.np)) {  // few waves have a row's label
+        const int at = (int)label - p_first;
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            if (at == 16 * i + n) e.zlabel[q] = acc[i][j][n];
+      }
       float2 t = make_float2(m, sum);
 #pragma unroll
       for (int o = 16; o < 64; o *= 2) t = join_stat(t, make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o)));

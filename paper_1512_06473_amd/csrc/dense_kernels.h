@@ -296,15 +296,15 @@ __global__ __launch_bounds__(256) void finish_loss_kernel(const float* __restric
   else write_loss(t, zlabel, label, e.classes, e.loss + q, e.lse_out + q);
 }
 
-// Joins the slots' maxima and sums of each row: ROWS rows by 256 / ROWS
+// Joins the slots' maxima and sums of each row: ROWS rows by THREADS / ROWS
 // threads, each of which takes every so many-th slot.
-template <int ROWS>
-static __global__ __launch_bounds__(256) void loss_kernel(const float2* __restrict__ stat,
+template <int ROWS, int THREADS>
+static __global__ __launch_bounds__(THREADS) void loss_kernel(const float2* __restrict__ stat,
                                                           const float* __restrict__ zlabel,
                                                           const long long* __restrict__ labels, int slots, int nq,
                                                           int classes, float* __restrict__ loss,
                                                           float* __restrict__ lse) {
-  constexpr int kEach = 256 / ROWS;
+  constexpr int kEach = THREADS / ROWS;
   __shared__ float2 part[kEach][ROWS];
   const int c = threadIdx.x % ROWS, r = threadIdx.x / ROWS, q = blockIdx.x * ROWS + c;
   float2 t = make_float2(-INFINITY, 0.f);
@@ -805,9 +805,9 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   // 16 rows read whole 128-byte lines; fewer than 64 rows would leave most of
   // the chip idle and go down hundreds of slots one after another.
   if (s.N >= 64)
-    loss_kernel<16><<<ceil_div(s.N, 16), 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
+    loss_kernel<16, 1024><<<ceil_div(s.N, 16), 1024, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
   else
-    loss_kernel<1><<<s.N, 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
+    loss_kernel<1, 256><<<s.N, 256, 0, st>>>(p.stat, p.zlabel, labels, slots, s.N, s.Ct, loss, lse);
   return hipGetLastError();
 }
 
