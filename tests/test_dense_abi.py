@@ -125,3 +125,26 @@ def test_python_refusals():
         api.linear_forward([1.0], w)
     with pytest.raises(ValueError):
         api._act("swish")
+
+
+def test_sizes_over_many_shapes(L):
+    """The host's planning for shapes of every magnitude: an answer, and not
+    beyond what copies, 256 MiB of a gradient and split sums come to."""
+    import random
+    rng = random.Random(5)
+    for _ in range(1500):
+        entry = rng.choice(list(CALLS))
+        dtype, s = rng.choice(((F32, 4), (BF16, 2), (F16, 2)))
+        N, Cs, Ct = (int(2 ** rng.uniform(0, b)) for b in (16, 14, 17))
+        args = dict(CALLS[entry], dtype=dtype, N=N, Cs=Cs, Ct=Ct)
+        for k, cols in (("ldx", Cs), ("ldy", Ct), ("lddy", Ct), ("ldr", Ct)):
+            if k in args:
+                args[k] = cols + rng.choice((0, 0, 1, 8))
+        if any(args.get(k) for k in ("pre", "y", "dx", "dw", "loss")):  # 1 TiB apart: none overlaps
+            args = {k: v << 8 if isinstance(v, int) and v >= at(1) else v for k, v in args.items()}
+        rc, n = size(getattr(L, entry), args.values())
+        assert rc == 0, (entry, args)
+        rows = 2 * Ct if "gated" in entry else Ct
+        copies = s * ((N + rows) * (Cs + 8) + N * (rows + 8))
+        sums = 4 * 513 * rows + 8 * N * (rows // 8 + 64) + 4 * 1024 * 65536 * 2 + 8 * N * (Cs + 8)
+        assert n <= copies + sums + (300 << 20), (entry, args, n)
