@@ -365,14 +365,19 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
  * Layouts: x [N][C_s], w [C_t][C_s], y, dy, residual [N][C_t].  x, y, dy and
  * residual have row strides ldx, ldy, lddy, ldr in elements (at least their
  * columns); everything else is contiguous.  Pointers are aligned to their
- * element.  Rows of whole 16 bytes at 16-byte aligned addresses are read in
- * place; otherwise x and w are first copied into the workspace.
+ * element.  Rows that start and end at whole dwords are read in place (always
+ * in fp32); otherwise, and for large 16-bit products whose rows do not end
+ * with whole 16 bytes, x and w are first copied into the workspace.  Calls of
+ * few rows copy nothing.
+ * Overlap: the range from an output's first element to its last, what lies
+ * between its rows included, meets no other argument's range (QCNN_ERR_ALIAS).
  * Limits: N <= 2^21; C_s, C_t (2 C_t of the gated layer) and strides <= 2^20;
  * no more than 2^22 tiles of 128 x 128 in any of the products
  * (QCNN_ERR_UNSUPPORTED past them).  Sizes are at least 1.
  * Workspace: with workspace_bytes NULL the library's per-stream workspace is
  * used.  With workspace NULL and workspace_bytes not NULL the call only
- * writes the size that it needs there (0: none) and launches nothing.  With
+ * writes the size that it needs there (0: none) and launches nothing; the
+ * size depends on all arguments, the pointers' alignment among them.  With
  * both, temporaries live in the caller's buffer of *workspace_bytes bytes
  * (256-byte aligned; QCNN_ERR_WORKSPACE if too small): for calls captured
  * into graphs that may run at the same time, each of which needs its own.

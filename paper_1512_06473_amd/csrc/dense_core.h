@@ -6,8 +6,8 @@
 // Each operand is stored along k ([rows][k], "C") or across it ([k][rows],
 // "S"): a forward pass is C x C, an input gradient S x C, a weight gradient
 // S x S.  A workgroup computes BP x BQ outputs; k runs in steps of 128 bytes.
-// Both tiles of a step go from memory straight to LDS (16 bytes per lane),
-// double-buffered, one barrier per step.
+// Both tiles of a step go from memory straight to LDS (16 bytes per lane; fp32:
+// through registers), two or four steps ahead, one barrier per step.
 //
 // A fragment is 16 bytes per lane: lane (g = lane / 16, i = lane % 16) holds
 // row i and the k's 8 g .. 8 g + 7 of 32 (16-bit types, one MFMA 16x16x32) or
@@ -76,7 +76,8 @@ struct Num16 {
   // slope's exponential with it (4096 x 4096 slopes: 45 us with erff).
   static __device__ __forceinline__ float phi(float z, float density) {
     const float t = __builtin_amdgcn_rcpf(1.f + 0.371231049f * fabsf(z));
-    const float tail = density * t * (0.148124367f + t * (0.14742066f + t * (0.134845033f + t * (0.0494158827f + t * (0.139162809f + t * (-0.166493893f + t * (0.0475246012f)))))));
+    const float upper = 0.0494158827f + t * (0.139162809f + t * (-0.166493893f + t * 0.0475246012f));
+    const float tail = density * t * (0.148124367f + t * (0.14742066f + t * (0.134845033f + t * upper)));
     return z > 0.f ? 1.f - tail : tail;
   }
 };
@@ -961,14 +962,18 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
   }
 
   // An infinity's lower parts are NaN: a tile whose sums are not all finite is
-  // computed again with fp32's own instruction, from fp32 tiles in LDS.
+  // computed again with fp32's own instruction, from fp32 tiles in LDS.  Past
+  // the columns of an S operand is whatever lies between its rows: it decides
+  // nothing.
+  const int end_p = PS ? a.np - t.cp - wp * WP - 4 * (lane >> 4) : BP;
+  const int end_q = QS ? a.nq - t.cq - wq * WQ - (lane & 15) : BQ;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < FP; ++i)
 #pragma unroll
     for (int j = 0; j < FQ; ++j)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) bad |= !(fabsf(acc[i][j][n]) < INFINITY);
+      for (int n = 0; n < 4; ++n) bad |= 16 * i + n < end_p && 16 * j < end_q && !(fabsf(acc[i][j][n]) < INFINITY);
   if (any_of_group(bad, reinterpret_cast<int*>(lds))) {
     typedef Operand<float, PS, BP, NW> OP;
     typedef Operand<float, QS, BQ, NW> OQ;

@@ -213,7 +213,7 @@ hipError_t run_slope(Slope a, void* dbias, const float* alpha, hipStream_t st) {
 
 // Sums of the parts of k, then the epilogue: a thread per quad of a row, or,
 // with many parts (few outputs, that is), G threads that take every G-th part
-// (24 x 4096 -> 500 gated, 32 parts: 25 us with one, 13 with four).
+// (24 x 4096 -> 500 gated, 32 parts: 25 us with one, 11 with four).
 template <typename T, int EPI, int G>
 __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ part, int splits, long long ldpart,
                                                      int np, int nq, int quads_of_row, const Epi e) {
@@ -596,7 +596,8 @@ struct Source {
   // tiles: the products read it; whole: and want the rows' ends, along k, to be
   // those of 16 bytes.
   Source(const void* ptr, long long ld_, int rows_, int cols_, Layout* l, bool tiles = true, bool whole = false)
-      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_), copy(tiles && (!direct<T>(ptr, ld_, cols_) || (whole && cols_ * sizeof(T) % 16)))  {
+      : p(static_cast<const T*>(ptr)), ld(ld_), rows(rows_), cols(cols_),
+        copy(tiles && (!direct<T>(ptr, ld_, cols_) || (whole && cols_ * sizeof(T) % 16))) {
     if (copy) at = l->add((size_t)rows * pad16<T>(cols) * sizeof(T));
   }
   hipError_t place(char* ws, hipStream_t st) {
@@ -653,8 +654,7 @@ hipError_t linear_forward(const LinearShape& s, const void* x, const void* w, co
   p.ldr = s.ldr;
   p.act = act;
   return c.template run<kLinear, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
-                                     std::min(wsrc.stored(), xs.stored()), p,
-                                                      reinterpret_cast<float*>(ws.get() + part), st);
+                   std::min(wsrc.stored(), xs.stored()), p, reinterpret_cast<float*>(ws.get() + part), st);
 }
 
 template <typename T>
@@ -679,8 +679,7 @@ hipError_t gated_forward(const LinearShape& s, const void* x, const void* w, con
   p.bias = bias;
   p.act = act;
   return c.template run<kGated, true>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
-                                     std::min(wsrc.stored(), xs.stored()), p,
-                                                    reinterpret_cast<float*>(ws.get() + part), st);
+                   std::min(wsrc.stored(), xs.stored()), p, reinterpret_cast<float*>(ws.get() + part), st);
 }
 
 // dx = dz w, as fp32 running sums in `acc` or finished in y.
@@ -800,8 +799,7 @@ hipError_t xent_forward(const LinearShape& s, const void* x, const void* w, cons
   p.loss = loss;
   p.lse_out = lse;
   e = c.template run<kStats, false>(wsrc.ptr(), wsrc.bytes(), xs.ptr(), xs.bytes(),
-                                     std::min(wsrc.stored(), xs.stored()), p,
-                                                  reinterpret_cast<float*>(ws.get() + part), st);
+                   std::min(wsrc.stored(), xs.stored()), p, reinterpret_cast<float*>(ws.get() + part), st);
   if (e != hipSuccess || slots == 0) return e;
   // 16 rows read whole 128-byte lines; fewer than 64 rows would leave most of
   // the chip idle and go down hundreds of slots one after another.
@@ -852,7 +850,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   float* scale = reinterpret_cast<float*>(ws.get() + scale_at);
   float* sums = reinterpret_cast<float*>(ws.get() + part);
   char* d = ws.get() + d_at;
-  const float gain = sizeof(T) == 2 && (float)(T)1e-7f == 1.1920929e-07f ? 1024.f : 1.f;  // fp16: 2^10
+  constexpr float gain = std::is_same<T, _Float16>::value ? 1024.f : 1.f;
   dmax_kernel<<<1, 1024, 0, st>>>(dloss, labels, s.N, gain, scale);
   e = hipGetLastError();
   for (int k = 0; k < pieces && e == hipSuccess; ++k) {

@@ -450,3 +450,97 @@ def test_rows_that_end_within_16_bytes(dev, tname, N, Cs, Ct):
     got = api.linear_forward(x, w)
     assert torch.equal(got[1], torch.copysign(torch.full_like(got[1], float("inf")), w[:, Cs - 1]))
     assert torch.isfinite(got[2:]).all()
+
+
+@pytest.mark.parametrize("tname", ["fp32", "bf16"])
+@pytest.mark.parametrize("N", [2500, 8])
+def test_rows_past_4_gib(dev, tname, N):
+    """Rows 2^20 elements apart, the largest stride: x, dy and y reach behind
+    2^32 bytes at 2500 rows (8: the few rows' kernel, the same strides)."""
+    T = TYPES[tname]
+    Cs, Ct, ld = 72, 40, 1 << 20
+    wide = torch.empty(N, ld, dtype=T, device=dev)
+    x, dy = wide[:, 1000:1000 + Cs], wide[:, -Ct:]
+    x.copy_(normal(dev, T, 1, N, Cs))
+    dy.copy_(normal(dev, T, 2, N, Ct))
+    w = normal(dev, T, 3, Ct, Cs)
+    out = torch.empty(N, ld, dtype=T, device=dev)[:, 17:17 + Ct]
+    print("rows past 4 GiB", tname, N, flush=True)
+    assert torch.equal(api.linear_forward(x, w, residual=dy, out=out),
+                       api.linear_forward(x.contiguous(), w, residual=dy.contiguous()))
+    for a, b in zip(api.linear_backward(dy, x, w), api.linear_backward(dy.contiguous(), x.contiguous(), w)):
+        assert torch.equal(a, b)
+    near(out.contiguous(), torch.mm(x.double(), w.double().t()) + dy.double(),
+         product_bound(Cs, torch.mm(x.double().abs(), w.double().abs().t()) + dy.double().abs(), out.double(), T), "y")
+
+
+@pytest.mark.parametrize("N", [5, 40])
+def test_classes_past_4_gib(dev, N):
+    """2^20 classes, the most: weights and their gradient reach behind 2^32 bytes."""
+    T, Cs, Ct = torch.bfloat16, 2304, 1 << 20
+    x, w = normal(dev, T, 1, N, Cs), normal(dev, T, 2, Ct, Cs, scale=1.0 / math.sqrt(Cs))
+    labels = torch.randint(Ct - 1000, Ct, (N,), generator=torch.Generator().manual_seed(3)).to(dev)
+    xd = x.double()
+    z = torch.cat([torch.mm(xd, p.double().t()) for p in w.split(1 << 17)], 1)
+    lse = torch.logsumexp(z, 1)
+    # a logit is off by 8 sqrt(C_s) 2^-24 of its products' magnitudes, less than sqrt(C_s) standard ones of 1 each
+    e = 8 * math.sqrt(Cs) * E32 * math.sqrt(Cs) + 32 * E32 * (1 + float(z.abs().max()))
+    print("classes past 4 GiB", N, flush=True)
+    loss, glse = api.linear_xent_forward(x, w, labels)
+    near(glse, lse, torch.full_like(lse, e), "lse")
+    near(loss, lse - z.gather(1, labels[:, None])[:, 0], torch.full_like(lse, 2 * e), "loss")
+    dloss = torch.full((N,), 1.0 / N, device=dev)
+    dx, dw, _ = api.linear_xent_backward(dloss, glse, x, w, labels)
+    last = slice(Ct - 1000, Ct)
+    d = torch.softmax(z, 1)
+    d.scatter_add_(1, labels[:, None], torch.full((N, 1), -1.0, device=dev, dtype=torch.float64))
+    d /= N
+    u = 2.0 ** -8  # d and the result are rounded to bf16
+    off = u * d.abs() + 2 * e * torch.softmax(z, 1) / N
+    for part in (last, slice(0, 1000)):
+        dp = d[:, part]
+        ref, A = torch.mm(dp.t(), xd), torch.mm(dp.t().abs(), xd.abs())
+        near(dw[part], ref, product_bound(N, A, ref, T) + torch.mm(off[:, part].t(), xd.abs()), "dw")
+    ref, A, E = (torch.zeros(N, Cs, dtype=torch.float64, device=dev) for _ in range(3))
+    for k, p in enumerate(w.split(1 << 17)):
+        cols, wd = slice(k << 17, (k + 1) << 17), p.double()
+        ref += torch.mm(d[:, cols], wd)
+        A += torch.mm(d[:, cols].abs(), wd.abs())
+        E += torch.mm(off[:, cols], wd.abs())
+    near(dx, ref, product_bound(Ct, A, ref, T) + E, "dx")
+
+
+@pytest.mark.parametrize("N", [8, 200])
+def test_fp32_parts_of_the_smallest_numbers(dev, N):
+    """Near 2^-122 the lower parts of a number are subnormal; large weights
+    bring the products back to ordinary size.  The parts below 2^-126 are at
+    most 2^-126 together, 2^-4 to 2^-24 of the largest, and each of them may be
+    dropped by hardware that does not keep subnormals: the sum's bound is then
+    C_s 2^-126 |w|."""
+    x, w = normal(dev, torch.float32, 1, N, 64), normal(dev, torch.float32, 2, 200, 64)
+    x *= 2.0 ** -100
+    x[1] *= 2.0 ** -22
+    w *= 2.0 ** 90
+    y = api.linear_forward(x, w)
+    ref = torch.mm(x.double(), w.double().t())
+    A = torch.mm(x.double().abs(), w.double().abs().t())
+    bound = 8 * 8 * E32 * A + 4 * E32 * ref.abs()
+    bound[1] += 2.0 ** -126 * w.double().abs().sum(1)
+    near(y, ref, bound, "small numbers")
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Cs,Ct", [(8, 72, 40), (300, 200, 130), (1030, 1000, 1030)])
+def test_what_lies_between_rows_decides_nothing(dev, tname, N, Cs, Ct):
+    """Bit for bit the same results with NaN, infinities or zeros there."""
+    T = TYPES[tname]
+    w, results = normal(dev, T, 3, Ct, Cs), []
+    for fill in (0.0, float("nan"), float("inf")):
+        wide_x = torch.full((N, Cs + 64), fill, dtype=T, device=dev)
+        wide_dy = torch.full((N, Ct + 64), fill, dtype=T, device=dev)
+        x, dy = wide_x[:, 8:8 + Cs], wide_dy[:, 16:16 + Ct]
+        x.copy_(normal(dev, T, 1, N, Cs))
+        dy.copy_(normal(dev, T, 2, N, Ct))
+        results.append([api.linear_forward(x, w, residual=dy), api.gated_forward(x, w), *api.linear_backward(dy, x, w)])
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
