@@ -851,10 +851,11 @@ struct Planes {
 };
 
 // Large tiles 256 x 128 (8 waves of 64 x 64), small ones 128 x 128 (of 64 x 32).
-// Bound by the matrix cores and power: 4096 x 4096 -> 4096 takes 680 us forward,
-// 612 and 598 for the gradients (200 to 230 TFLOP/s; fp32's own instruction
-// 970, split where the fragments are read 712 to 765), matrix cores busy for 60
-// % of the cycles.
+// Bound by the matrix cores and power: 4096 x 4096 -> 4096 takes 670 us forward,
+// 608 and 585 for the gradients (205 to 235 TFLOP/s, that is 1230 to 1410 of
+// bf16 products).  Fp32's own instruction 970, split where the fragments are
+// read 712 to 765, split in blocks before and after the products of a row 720,
+// 625 and 617.
 template <bool PS, bool QS, int BP, int BQ, int WP, int WQ, int EPI, bool GATED>
 __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel(const Prod a, const Epi e) {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -862,9 +863,9 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
   static_assert(!GATED || !PS, "the gated layer's weights are read along k");
   typedef Planes<PS, BP, NW> LP;
   typedef Planes<QS, BQ, NW> LQ;
-  constexpr int kBuffer = LP::kBytes + LQ::kBytes;
-  constexpr int kLds = 2 * kBuffer > NW * kRoomBytes ? 2 * kBuffer : NW * kRoomBytes;
-  __shared__ __align__(16) char lds[kLds];
+  // Two arrays: the compiler then knows that reads of one may pass writes of
+  // the other.
+  __shared__ __align__(16) char lds[LP::kBytes + LQ::kBytes], other[LP::kBytes + LQ::kBytes];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NWP, wq = wave / NWP;
@@ -896,14 +897,8 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
       ahead[j] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(descriptor(walk_q, step, none), v, 0, 0));
     }
   };
-  auto put = [&](char* buffer, int s, int j) __attribute__((always_inline)) {
+  auto put = [&](char* buffer, int j) __attribute__((always_inline)) {
     const bool is_p = j < LP::kLoads;
-    if ((is_p ? !PS : !QS) && t.ragged && s + 1 == t.nsteps) {  // what lies behind a row's end
-      const int left = walk_p.left(t.step0 + s), chunk = is_p ? walk_p.chunk : walk_q.chunk;
-#pragma unroll
-      for (int i = 1; i < 4; ++i)
-        if (chunk + 4 * i >= left) ahead[j][i] = 0.f;
-    }
     char* o = is_p ? buffer + LP::write_at(write_p, j) : buffer + LP::kBytes + LQ::write_at(write_q, j - LP::kLoads);
     uint2 w[3];
     split_bf16(ahead[j], w);
@@ -911,17 +906,29 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
     for (int n = 0; n < 3; ++n) *reinterpret_cast<uint2*>(o + n * (is_p ? LP::kPlane : LQ::kPlane)) = w[n];
   };
 
+  // What lies behind the rows' ends, and came with their last 16 bytes.
+  auto cut_off = [&](char* buffer) __attribute__((always_inline)) {
+    const int id = threadIdx.x;
+    const bool is_p = id < BP;
+    const int r = is_p ? id : id - BP;
+    if (is_p ? PS : QS || r >= BQ) return;
+    char* row = buffer + (is_p ? 0 : LP::kBytes) + r * 64;
+    for (int k = walk_p.left(t.step0 + t.nsteps - 1) / 4; k & 3; ++k)
+#pragma unroll
+      for (int n = 0; n < 3; ++n)
+        *reinterpret_cast<uint16_t*>(row + n * (is_p ? LP::kPlane : LQ::kPlane) + (((k >> 3) ^ LP::spread(r)) << 4) +
+                                     (k & 7) * 2) = 0;
+  };
+
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) load(0, j);
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
-    put(lds, 0, j);
+    put(lds, j);
     load(1, j);
   }
   meet();
-  for (int s = 0; s < t.nsteps; ++s) {
-    const char* now = lds + (s & 1) * kBuffer;
-    char* next = lds + (~s & 1) * kBuffer;
+  auto body = [&](auto last, int s, const char* now, char* next) __attribute__((always_inline)) {
     b8 fq[FQ][3], fp[2][3];
 #pragma unroll
     for (int n = 0; n < 3; ++n) fp[0][n] = LP::frag(now + n * LP::kPlane, read_p, 0);
@@ -929,16 +936,8 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
     for (int j = 0; j < FQ; ++j)
 #pragma unroll
       for (int n = 0; n < 3; ++n) fq[j][n] = LQ::frag(now + LP::kBytes + n * LQ::kPlane, read_q, j);
-    // Half of the next step's numbers while those come, the others after the
-    // products of the rows.
-    constexpr int kFirst = kLoads / 2;
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < kFirst; ++j) {
-      put(next, s + 1, j);
-      load(s + 2, j);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    // The next step's numbers and the loads of the one after, between the
+    // products, which leave three of four issue slots.
 #pragma unroll
     for (int i = 0; i < FP; ++i) {
       if (i + 1 < FP) {
@@ -952,14 +951,47 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
         for (int j = 0; j < FQ; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i & 1][kA[n]], fq[j][kB[n]], acc[i][j], 0, 0, 0);
       }
+      if constexpr (!decltype(last)::value) {
 #pragma unroll
-      for (int j = kFirst + i * (kLoads - kFirst) / FP; j < kFirst + (i + 1) * (kLoads - kFirst) / FP; ++j) {
-        put(next, s + 1, j);
-        load(s + 2, j);
+        for (int j = i * kLoads / FP; j < (i + 1) * kLoads / FP; ++j) {
+          put(next, j);
+          load(s + 2, j);
+        }
       }
     }
+    constexpr int kReadsP = 3 * (PS ? 2 : 1), kReadsQ = 3 * (QS ? 2 : 1), kRow = 6 * FQ, kMma = kRow * FP;
+    constexpr int kEach = kMma / kLoads, kFill = (28 * kLoads + kMma - 1) / kMma;
+    __builtin_amdgcn_sched_group_barrier(0x100, kReadsP + FQ * kReadsQ, 0);
+#pragma unroll
+    for (int m = 0; m < kMma; ++m) {
+      if (m % kRow == 0 && m / kRow + 1 < FP) __builtin_amdgcn_sched_group_barrier(0x100, kReadsP, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (decltype(last)::value) continue;
+      __builtin_amdgcn_sched_group_barrier(0x002, kFill, 0);
+      if (m % kEach == kEach - 1) {
+        __builtin_amdgcn_sched_group_barrier(0x200, 3, 0);
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    meet();
+  };
+  const std::false_type more;
+  int s = 0;
+  for (; s + 2 < t.nsteps; s += 2) {
+    body(more, s, lds, other);
+    body(more, s + 1, other, lds);
+  }
+  char* end = lds;
+  if (s + 2 == t.nsteps) {
+    body(more, s, lds, other);
+    end = other;
+  }
+  if ((!PS || !QS) && t.ragged) {
+    cut_off(end);
     meet();
   }
+  body(std::true_type(), 0, end, nullptr);
 
   // An infinity's lower parts are NaN: a tile whose sums are not all finite is
   // computed again with fp32's own instruction, from fp32 tiles in LDS.  Past
@@ -1014,8 +1046,11 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel
       wait_and_meet<0>();
     }
   }
-  finish_tile<float, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, reinterpret_cast<f4*>(lds + wave * kRoomBytes), lane, wp,
-                                              wq);
+  constexpr int kRoom = WP * WQ * 4 < kRoomBytes ? WP * WQ * 4 : kRoomBytes;
+  static_assert(NW / 2 * kRoom <= LP::kBytes + LQ::kBytes, "half of the waves' rooms in an array");
+  static_assert(BP * 128 + BQ * 128 <= LP::kBytes + LQ::kBytes, "fp32 tiles in an array");
+  f4* const room = reinterpret_cast<f4*>((wave < NW / 2 ? lds : other) + wave % (NW / 2) * kRoom);
+  finish_tile<float, WP, WQ, NWP, EPI, GATED>(a, e, t, acc, room, lane, wp, wq);
 #endif
 }
 
