@@ -340,10 +340,17 @@ struct Prod {
   long long ldpart;     // kGated's sums: gate at p, up at ldpart / 2 + p
 };
 
+__device__ __forceinline__ int bytes_of(long long bytes) {
+  const int low = (int)bytes, high = (int)(bytes >> 32);  // scalar compares have 32 bits
+  return high < 0 ? 0 : high > 0 || low < 0 ? 0x7fffffff : low;
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const char* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000);
+}
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const char* base, long long bytes) {
-  const long long cap = 0x7fffffffLL;
-  const int num = (int)(bytes < 0 ? 0 : bytes > cap ? cap : bytes);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, num, 0x00020000);
+  return resource(base, bytes_of(bytes));
 }
 
 // An operand's tile of ROWS rows: staging and fragments.
@@ -491,7 +498,7 @@ struct Walk {
     return S ? (long long)step * O::kStep * ld : (long long)step * 128;
   }
   // Bytes of k that a C operand has in this step.
-  __device__ __forceinline__ int left(int step) const { return (int)min(kbytes - (long long)step * 128, 128LL); }
+  __device__ __forceinline__ int left(int step) const { return min((int)kbytes - step * 128, 128); }
 
   // Offset of load j's 16 bytes; row: the load's first in the tile.
   __device__ __forceinline__ int offset(int row, int delta, int left) const {
@@ -659,15 +666,18 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
 // (256 x 256, 8 waves of 128 x 64): a step is 64 MFMA per wave for 24 LDS reads
 // of 16 bytes and 8 loads; a larger tile than 128 x 128 halves the LDS and L2
 // bytes per product, and 64 KB a step twice is what LDS holds.  Bound by the
-// matrix cores and the chip's power: 8192 x 4096 -> 16384 in bf16 takes 850 us
-// (1290 TFLOP/s), its input gradient 830, its weight gradient 840, with the
-// matrix cores busy for 61, 67 and 65 % of the cycles at 1.6 to 2 GHz; the same
-// products of zeros run at 1390 to 1530 TFLOP/s.  Without the half-step
-// prefetch 1128 us, results stored in the products' order (not through LDS)
-// 1060; 128 x 128 tiles 1185.  Four waves of 128 x 128 spill their sums between
-// the two register files (1140 us); 32 x 32 MFMA are 5 % slower.
+// matrix cores and the chip's power: 8192 x 4096 -> 16384 in bf16 takes 825 us
+// (1330 TFLOP/s), its input gradient 790, its weight gradient 815, at 1.6 to 2
+// GHz.  Without the half-step prefetch 1128 us, results stored in the products'
+// order (not through LDS) 1060, 128 x 128 tiles 1185; with a step's scalar work
+// and loads in a block behind the barrier 865, not between the products.  Four
+// waves of 128 x 128 spill their sums between the two register files (1140 us);
+// 32 x 32 MFMA are 5 % slower.
+// Bounded to 512 threads also where 256 run: with more than 256 registers to
+// give, the compiler keeps the sums in the other file and moves them around in
+// every turn of the loop (512 x 4096 -> 4096: 29.2 us, so 28.2).
 template <typename T, bool PS, bool QS, int BP, int BQ, int WP, int WQ, int DEPTH, int EPI, bool GATED>
-__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(const Prod a, const Epi e) {
+__global__ __launch_bounds__(512) void product_kernel(const Prod a, const Epi e) {
 #ifdef __HIP_DEVICE_COMPILE__  // the host pass, which only needs the name, gives up on the body without a word
   constexpr int NWP = BP / WP, NW = NWP * (BQ / WQ), FP = WP / 16, FQ = WQ / 16;
   static_assert(!GATED || !PS, "the gated layer's weights are read along k");
@@ -688,27 +698,47 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   const Place t = place_of<GATED ? BP / 2 : BP, BQ, sizeof(T)>(a);
   const int nsteps = t.nsteps;
   // Large tiles have no registers left for it: their rows end with 16 bytes.
-  const bool ragged = BP == 128 && (!PS || !QS) && t.ragged;
+  constexpr bool kCut = BP == 128 && (!PS || !QS);
+  const bool ragged = kCut && t.ragged;
   const Walk<T, PS, BP, NW> walk_p(a.p, a.ldp, t.cp, a.np, a.colsp, a.nk, a.kp, wave, lane, true);
   const Walk<T, QS, BQ, NW> walk_q(a.q, a.ldq, t.cq, a.nq, a.colsq, a.nk, a.kq, wave, lane, true);
 
-  auto stage = [&](int s, char* lp, char* lq) __attribute__((always_inline)) {
+  // Where a step's bytes lie; made ahead of its loads, in scalar registers,
+  // except where both operands are read transposed: the order that this needs
+  // costs large tiles eight vector registers too many (their loop spills:
+  // weight gradient of 8192 x 4096 -> 16384, 1690 us for 815).
+  constexpr bool kAhead = !PS || !QS;
+  struct Source {
+    const char *p, *q;
+    int np, nq, left;
+  };
+  auto locate = [&](int s) __attribute__((always_inline)) {
     const int step = t.step0 + s;
     const bool none = s >= nsteps;  // loads nothing: the loop runs ahead of its end
-    const __amdgpu_buffer_rsrc_t rq = descriptor(walk_q, step, none), rp = descriptor(walk_p, step, none);
-    const __amdgpu_buffer_rsrc_t rp2 = GATED ? descriptor(walk_p, step, none, a.p2) : rp;
-    const int left = walk_p.left(step);
+    const long long bp = walk_p.before(step), bq = walk_q.before(step);
+    Source r;
+    r.p = walk_p.base + bp;
+    r.q = walk_q.base + bq;
+    r.np = bytes_of(none ? 0 : walk_p.extent - bp);
+    r.nq = bytes_of(none ? 0 : walk_q.extent - bq);
+    r.left = walk_p.left(step);
+    if (kAhead) asm volatile("" : "+s"(r.p), "+s"(r.q), "+s"(r.np), "+s"(r.nq), "+s"(r.left));
+    return r;
+  };
+  auto stage = [&](const Source& r, char* lp, char* lq) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rq = resource(r.q, r.nq), rp = resource(r.p, r.np);
+    const __amdgpu_buffer_rsrc_t rp2 = GATED ? resource(r.p + a.p2 * walk_p.ld, r.np) : rp;
 #pragma unroll
     for (int j = 0; j < OP::kLoads; ++j) {
-      const int r = OP::first(wave, j);
-      const int v = walk_p.offset(GATED ? gated_row<WP>(r) : r, OP::chunk_delta(j), left);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && gated_up<WP>(r) ? rp2 : rp,
+      const int row = OP::first(wave, j);
+      const int v = walk_p.offset(GATED ? gated_row<WP>(row) : row, OP::chunk_delta(j), r.left);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(GATED && gated_up<WP>(row) ? rp2 : rp,
                                                (lds_void*)(lp + (wave + j * NW) * 1024), 16, v, 0, 0, 0);
     }
 #pragma unroll
     for (int j = 0; j < OQ::kLoads; ++j)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)(lq + (wave + j * NW) * 1024), 16,
-                                               walk_q.offset(OQ::first(wave, j), OQ::chunk_delta(j), left), 0, 0, 0);
+                                               walk_q.offset(OQ::first(wave, j), OQ::chunk_delta(j), r.left), 0, 0, 0);
   };
 
   f4 acc[FP][FQ];
@@ -737,20 +767,20 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
       for (int j = 0; j < FQ; ++j) acc[i][j] = Num<T>::mma(f.p[i], f.q[j], acc[i][j]);
   };
   // LDS reads, and a step's loads, one by one between the products.
-  auto interleave = [](auto loads_) __attribute__((always_inline)) {
+  auto interleave = [&](auto loads_) __attribute__((always_inline)) {
     constexpr int reads = FP * OP::kReads + FQ * OQ::kReads, mmas = FP * FQ;
-    constexpr int loads = decltype(loads_)::value, n = reads > loads ? reads : loads;
+    constexpr int loads = decltype(loads_)::value;
     constexpr int per = mmas / (reads + loads) > 0 ? mmas / (reads + loads) : 1;
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      if (i < reads) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-      }
-      if (i < loads) {
-        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
-      }
+    for (int i = 0; i < loads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < reads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, per, 0);
+      if (kAhead && loads == 0) __builtin_amdgcn_sched_group_barrier(0x004, 3, 0);
     }
     constexpr int rest = mmas - per * (reads + loads);
     if (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
@@ -761,17 +791,18 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   // further on is sent for, and the next step's first half is read under the
   // second half's products.
   Frags f0, f1;
-  auto body = [&](int s, char* lp, char* lq, char* next_p, char* next_q) __attribute__((always_inline)) {
+  auto body = [&](auto cut, int s, char* lp, char* lq, char* next_p, char* next_q) __attribute__((always_inline)) {
     read(f1, lp, lq, 1);
     multiply(f0);
+    const Source far = locate(s + DEPTH);
     interleave(std::integral_constant<int, 0>());
     __builtin_amdgcn_sched_barrier(0);
     wait_and_meet<(DEPTH - 2) * kFlight>();
-    if (ragged && s + 2 == nsteps) {
+    if (decltype(cut)::value && ragged && s + 2 == nsteps) {
       zero_tail<PS, QS, BP, BQ>(next_p, next_q, walk_p.left(t.step0 + s + 1), wave);
       meet();
     }
-    stage(s + DEPTH, lp, lq);
+    stage(far, lp, lq);
     read(f0, next_p, next_q, 0);
     multiply(f1);
     interleave(std::integral_constant<int, kFlight>());
@@ -779,21 +810,27 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_kernel(con
   };
 
 #pragma unroll
-  for (int b = 0; b < DEPTH; ++b) stage(b, ps[b], qs[b]);
+  for (int b = 0; b < DEPTH; ++b) stage(locate(b), ps[b], qs[b]);
   wait_and_meet<(DEPTH - 1) * kFlight>();
   if (ragged && nsteps == 1) {
     zero_tail<PS, QS, BP, BQ>(p0, q0, walk_p.left(t.step0), wave);
     meet();
   }
   read(f0, p0, q0, 0);
+  // A branch within the loop would part what is to be interleaved: the steps
+  // that may have to cut are behind it.
+  constexpr int kRest = kCut ? DEPTH + 1 : DEPTH - 1;
   int s = 0;
-  for (; s + DEPTH <= nsteps; s += DEPTH) {
+  for (; s + DEPTH + (kCut ? 2 : 0) <= nsteps; s += DEPTH) {
 #pragma unroll
-    for (int b = 0; b < DEPTH; ++b) body(s + b, ps[b], qs[b], ps[(b + 1) % DEPTH], qs[(b + 1) % DEPTH]);
+    for (int b = 0; b < DEPTH; ++b)
+      body(std::false_type(), s + b, ps[b], qs[b], ps[(b + 1) % DEPTH], qs[(b + 1) % DEPTH]);
   }
 #pragma unroll
-  for (int b = 0; b < DEPTH - 1; ++b)
-    if (s + b < nsteps) body(s + b, ps[b], qs[b], ps[b + 1], qs[b + 1]);
+  for (int b = 0; b < kRest; ++b)
+    if (s + b < nsteps)
+      body(std::integral_constant<bool, kCut>(), s + b, ps[b % DEPTH], qs[b % DEPTH], ps[(b + 1) % DEPTH],
+           qs[(b + 1) % DEPTH]);
   wait_and_meet<0>();  // nothing is on its way to this LDS, or read from it, any more
 
   constexpr int kPer = OP::kBytes / kRoomBytes;  // waves' rooms in a tile
