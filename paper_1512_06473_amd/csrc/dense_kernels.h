@@ -172,23 +172,26 @@ __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
   }
 }
 
-// out[c] = alpha sum_r part[r][c]: 64 columns by 4 groups of rows.
+// out[c] = alpha sum_r part[r][c]: 64 columns by 16 groups of rows (512 rows of
+// 4096 sums: 7.0 us with 4 groups, 4.8 with 16).
 template <typename T>
-__global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ part, int rows, long long width,
-                                                     const float* alpha, T* __restrict__ out) {
-  __shared__ float group[4][64];
+__global__ __launch_bounds__(1024) void colsum_kernel(const float* __restrict__ part, int rows, long long width,
+                                                      const float* alpha, T* __restrict__ out) {
+  constexpr int kGroups = 16;
+  __shared__ float group[kGroups][64];
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
   const long long c = blockIdx.x * 64LL + lane;
   float s = 0.f;
   if (c < width) {
 #pragma unroll 8
-    for (int r = g; r < rows; r += 4) s += part[r * width + c];
+    for (int r = g; r < rows; r += kGroups) s += part[r * width + c];
   }
   group[g][lane] = s;
-  __syncthreads();
-  if (g != 0 || c >= width) return;
-  s = (s + group[1][lane]) + (group[2][lane] + group[3][lane]);
-  out[c] = (T)(alpha ? s * *alpha : s);
+  for (int n = kGroups / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (g < n) group[g][lane] = s += group[g + n][lane];
+  }
+  if (g == 0 && c < width) out[c] = (T)(alpha ? s * *alpha : s);
 }
 
 // Rows of a thread: all of a few, which saves the kernel that joins the sums;
@@ -199,7 +202,7 @@ inline int slope_chunk(int rows) { return rows <= 16 ? rows : std::max(4, ceil_d
 template <typename T, bool GATED>
 hipError_t run_slope(Slope a, void* dbias, const float* alpha, hipStream_t st) {
   const int chunks = ceil_div(a.rows, a.chunk), width = GATED ? 2 * a.cols : a.cols;
-  const int threads = ceil_div(a.cols, 16 / (int)sizeof(T)) + 1;
+  const int threads = ceil_div(a.cols, 16 / (int)sizeof(T)) + (a.dz && a.lddz > width);
   if (chunks == 1) {
     a.sums = dbias;
     a.alpha = alpha;
@@ -207,7 +210,7 @@ hipError_t run_slope(Slope a, void* dbias, const float* alpha, hipStream_t st) {
   slope_kernel<T, GATED><<<dim3(ceil_div(threads, 256), chunks), 256, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !dbias || chunks == 1) return e;
-  colsum_kernel<T><<<ceil_div(width, 64), 256, 0, st>>>(a.part, chunks, width, alpha, static_cast<T*>(dbias));
+  colsum_kernel<T><<<ceil_div(width, 64), 1024, 0, st>>>(a.part, chunks, width, alpha, static_cast<T*>(dbias));
   return hipGetLastError();
 }
 
