@@ -201,6 +201,33 @@ __device__ __forceinline__ void store_quad(T* p, f4 v, int n) {
   }
 }
 
+// 16 bytes of elements, or the n that are left.
+template <typename T, int Q>
+__device__ __forceinline__ void load_wide(const T* p, int n, f4 (&v)[Q]) {
+  if (n >= 4 * Q) {
+    typename Num<T>::Frag t;
+    __builtin_memcpy(&t, p, 16);
+#pragma unroll
+    for (int i = 0; i < 4 * Q; ++i) v[i / 4][i % 4] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int k = 0; k < Q; ++k) v[k] = load_quad(p + 4 * k, n - 4 * k);
+  }
+}
+
+template <typename T, int Q>
+__device__ __forceinline__ void store_wide(T* p, int n, const f4 (&v)[Q]) {
+  if (n >= 4 * Q) {
+    typename Num<T>::Frag t;
+#pragma unroll
+    for (int i = 0; i < 4 * Q; ++i) t[i] = (T)v[i / 4][i % 4];
+    __builtin_memcpy(p, &t, 16);
+  } else {
+#pragma unroll
+    for (int k = 0; k < Q; ++k) store_quad(p + 4 * k, v[k], n - 4 * k);
+  }
+}
+
 // The bias of columns p .. p + 3 (zeros without one, and past the end).
 template <typename T>
 __device__ __forceinline__ f4 bias_quad(const Epi& e, int np, int p, int from = 0) {

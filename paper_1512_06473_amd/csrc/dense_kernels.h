@@ -73,33 +73,6 @@ struct Slope {
   int rows, cols, chunk, act;  // cols: of dy
 };
 
-// 16 bytes of elements, or the n that are left.
-template <typename T, int Q>
-__device__ __forceinline__ void load_wide(const T* p, int n, f4 (&v)[Q]) {
-  if (n >= 4 * Q) {
-    typename Num<T>::Frag t;
-    __builtin_memcpy(&t, p, 16);
-#pragma unroll
-    for (int i = 0; i < 4 * Q; ++i) v[i / 4][i % 4] = (float)t[i];
-  } else {
-#pragma unroll
-    for (int k = 0; k < Q; ++k) v[k] = load_quad(p + 4 * k, n - 4 * k);
-  }
-}
-
-template <typename T, int Q>
-__device__ __forceinline__ void store_wide(T* p, int n, const f4 (&v)[Q]) {
-  if (n >= 4 * Q) {
-    typename Num<T>::Frag t;
-#pragma unroll
-    for (int i = 0; i < 4 * Q; ++i) t[i] = (T)v[i / 4][i % 4];
-    __builtin_memcpy(p, &t, 16);
-  } else {
-#pragma unroll
-    for (int k = 0; k < Q; ++k) store_quad(p + 4 * k, v[k], n - 4 * k);
-  }
-}
-
 // With GROUPS, that many groups of a block's threads share its rows.
 template <typename T, bool GATED, int GROUPS>
 __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
@@ -745,6 +718,21 @@ Prod dw_prod(const Source<T>& x, const char* dz, long long lddz, int stored, int
   return a;
 }
 
+// Weight gradients of at most 32 rows, one k of the matrix instruction: their
+// own kernel (4096 -> 16384 in us: 32 rows bf16 36, fp32 75; tiles, at 33 rows,
+// 52 and 100; 512 -> 512 takes 11 to 12 either way).
+inline bool few_outer(int N) { return N <= 32; }
+
+template <typename T>
+hipError_t run_outer(const Source<T>& x, const char* d, long long ldd, int rows, const Epi& e, hipStream_t st) {
+  Outer a = {x.ptr(), d, static_cast<char*>(e.y), x.ld, ldd, x.rows, x.cols, rows, 0, e.alpha};
+  // 8192 waves fill the chip; each reads its columns of x once.
+  const int across = ceil_div(x.cols, 512), down = std::max(1, std::min(ceil_div(rows, 16), 2048 / across));
+  a.per = ceil_div(ceil_div(rows, down), 16) * 16;
+  LaunchTimer timer;
+  return timed_launch(&timer, outer_kernel<T>, dim3(across, ceil_div(rows, a.per)), dim3(256), 0u, st, a);
+}
+
 // Both layers' gradients from dz: rows of the weight `rows` (2 C_t if gated).
 template <typename T, bool GATED>
 hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, const void* w, const void* pre, int act,
@@ -760,8 +748,9 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
   const size_t dz_at = in_place ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
   const int chunk = slope_chunk(s.N), chunks = ceil_div(s.N, chunk);
   const size_t sums_at = dbias ? l.add((size_t)chunks * rows * 4) : 0;
-  Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
-  const size_t part = l.add(std::max(dx ? cx.part_bytes : 0, dw ? cw.part_bytes : 0));
+  const bool outer = few_outer(s.N);
+  Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l, !outer), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
+  const size_t part = l.add(std::max(dx ? cx.part_bytes : 0, dw && !outer ? cw.part_bytes : 0));
   Scratch ws;
   bool asked;
   hipError_t e = claim(&ws, l, room, st, &asked);
@@ -798,7 +787,8 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Epi p = {};
     p.y = dw;
     p.ldy = s.Cs;
-    e = run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, stored, rows), p, cw, sums, st);
+    e = outer ? run_outer<T>(xs, dz, lddz, rows, p, st)
+              : run_product<T, true, true, kLinear, false>(dw_prod(xs, dz, lddz, stored, rows), p, cw, sums, st);
   }
   return e;
 }
@@ -850,12 +840,13 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   if (fit < 256) fit = 256;
   const int piece = fit < s.Ct ? (int)fit : s.Ct, pieces = ceil_div(s.Ct, piece);
   bool tiles = false, whole = false;
+  const bool outer = few_outer(s.N);
   for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
     const Forward<T> f(n, s.N, s.Cs, false);
     tiles |= !f.few;
     whole |= f.whole();
   }
-  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, tiles || dw, whole), wsrc(w, s.Cs, s.Ct, s.Cs, &l, tiles || dx, whole);
+  Source<T> xs(x, s.ldx, s.N, s.Cs, &l, tiles || (dw && !outer), whole), wsrc(w, s.Cs, s.Ct, s.Cs, &l, tiles || dx, whole);
   const long long ldd = pad16<T>(piece), ldacc = (s.Cs + 3) / 4 * 4;
   const size_t d_at = l.add((size_t)s.N * ldd * sizeof(T)), scale_at = l.add(8);
   const size_t acc_at = dx && pieces > 1 ? l.add((size_t)s.N * ldacc * 4) : 0;
@@ -865,7 +856,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
     part_bytes = std::max(part_bytes, Forward<T>(n, s.N, s.Cs, false).part_bytes);
     if (dx) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, s.N, pad16<T>(n), false).part_bytes);
-    if (dw) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, n, s.N, false).part_bytes);
+    if (dw && !outer) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, n, s.N, false).part_bytes);
   }
   const size_t part = l.add(part_bytes);
   Scratch ws;
@@ -926,8 +917,9 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       o.y = static_cast<T*>(dw) + (long long)c0 * s.Cs;
       o.ldy = s.Cs;
       o.alpha = scale + 1;
-      e = run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, (int)ld, n), o, cut_of<T>(s.Cs, n, s.N, false), sums,
-                                                     st);
+      e = outer ? run_outer<T>(xs, d, ld, n, o, st)
+                : run_product<T, true, true, kLinear, false>(dw_prod(xs, d, ld, (int)ld, n), o,
+                                                             cut_of<T>(s.Cs, n, s.N, false), sums, st);
     }
   }
   return e;

@@ -544,3 +544,28 @@ def test_what_lies_between_rows_decides_nothing(dev, tname, N, Cs, Ct):
         results.append([api.linear_forward(x, w, residual=dy), api.gated_forward(x, w), *api.linear_backward(dy, x, w)])
     for other in results[1:]:
         assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N", [1, 15, 16, 17, 31, 32, 33])
+@pytest.mark.parametrize("Cs,Ct", [(1, 1), (127, 31), (129, 4100), (1025, 333), (5000, 20)])
+def test_weight_gradients_of_few_rows(dev, tname, N, Cs, Ct):
+    """Both sides of the switch between the kernels, odd sizes, rows of x and dy
+    at odd places; and the guard behind dw stays as it was."""
+    T = TYPES[tname]
+    wide_x = torch.full((N, Cs + 3), float("nan"), dtype=T, device=dev)
+    wide_dy = torch.full((N, Ct + 5), float("nan"), dtype=T, device=dev)
+    x, dy = wide_x[:, 1:1 + Cs], wide_dy[:, 3:3 + Ct]
+    x.copy_(normal(dev, T, 1, N, Cs))
+    dy.copy_(normal(dev, T, 2, N, Ct))
+    print("few rows", tname, N, Cs, Ct, flush=True)
+    flat = torch.full((Ct * Cs + 64,), 7.0, dtype=T, device=dev)
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[T]
+    rc = lib().qcnn_linear_backward(code, dy.data_ptr(), Ct + 5, x.data_ptr(), Cs + 3, N, Cs, None, Ct, None, 0, None,
+                                    flat.data_ptr(), None, None, None, torch.cuda.current_stream(dev).cuda_stream)
+    assert rc == 0
+    ref, A = torch.mm(dy.double().t(), x.double()), torch.mm(dy.double().abs().t(), x.double().abs())
+    # below 2^-14 fp16's numbers are 2^-24 apart: half a step is 2^-25, not 2^-11 of the value
+    bound = product_bound(N, A, ref, T) + (2.0 ** -25 if T == torch.float16 else 0)
+    near(flat[:Ct * Cs].view(Ct, Cs), ref, bound, "dw")
+    assert (flat[Ct * Cs:] == 7).all()
