@@ -367,8 +367,8 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
  * columns); everything else is contiguous.  Pointers are aligned to their
  * element.  Rows that start and end at whole dwords are read in place (always
  * in fp32); otherwise, and for large 16-bit products whose rows do not end
- * with whole 16 bytes, x and w are first copied into the workspace.  Calls of
- * few rows copy nothing.
+ * with whole 16 bytes, x and w are first copied into the workspace.  Forward
+ * calls of few rows copy nothing.
  * Overlap: the range from an output's first element to its last, what lies
  * between its rows included, meets no other argument's range (QCNN_ERR_ALIAS).
  * Limits: N <= 2^21; C_s, C_t (2 C_t of the gated layer) and strides <= 2^20;
