@@ -259,5 +259,101 @@ __global__ __launch_bounds__(256) void outer_kernel(const Outer a) {
   }
 }
 
+// Input gradients of few rows in fp32: y[n][c] = sum_t d[n][t] w[t][c], n <= 32.
+// Bound by reading w (1 x 3968 -> 61184: 179 us, 5.4 TB/s, with large tiles 289),
+// past 16 rows by fp32's own matrix instruction (32 rows 268, tiles, at 33,
+// 286; 4096 -> 16384 77 and 78).  A lane's 16 bytes of a row are four columns,
+// each for a matrix instruction of its own, which therefore takes every fourth
+// of 64 columns; 16 rows t are four loads.  A workgroup's waves have parts of
+// t, which meet in LDS.
+struct Thin {
+  const float* w;
+  const float* d;
+  long long ldw, ldd;  // elements
+  int rows, cols, n;   // rows: of w
+  int units, splits;   // 16 rows each, of a wave; workgroups along t
+  float* part;
+  long long ldpart;
+};
+
+template <int FQ, int EPI>
+static __global__ __launch_bounds__(64 * kFewWaves) void thin_kernel(const Thin a, const Epi e) {
+  __shared__ f4 parts[kFewWaves][4 * FQ][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, i = lane & 15;
+  const int tp = blockIdx.x / a.splits, split = blockIdx.x % a.splits, c0 = tp * 64, c = c0 + 4 * i;
+  const int all = (a.rows + 15) / 16;
+  const int u0 = min(all, (split * kFewWaves + wave) * a.units), u1 = min(all, u0 + a.units);
+  f4 acc[4][FQ];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[k][j] = f4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const f4 (&w)[4], const f4 (&d)[FQ]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j)
+          acc[k][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[m][k], d[j][m], acc[k][j], 0, 0, 0);
+  };
+  // Past the last n, column or row: zeros.
+  auto load = [&](int u, bool whole, f4 (&w)[4], f4 (&d)[FQ]) __attribute__((always_inline)) {
+    const int t = 16 * u + 4 * g;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      w[m] = f4{0.f, 0.f, 0.f, 0.f};
+      if (whole || t + m < a.rows) w[m] = load_quad(a.w + (t + m) * a.ldw + c, a.cols - c);
+    }
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int n = 16 * j + i;
+      d[j] = f4{0.f, 0.f, 0.f, 0.f};
+      if (n < a.n) d[j] = load_quad(a.d + n * a.ldd + t, whole ? 4 : a.rows - t);
+    }
+  };
+  const int full = min(u1, a.rows / 16);
+  int u = u0;
+  for (; u + 2 <= full; u += 2) {
+    f4 w[2][4], d[2][FQ];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) load(u + b, true, w[b], d[b]);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) multiply(w[b], d[b]);
+  }
+  for (; u < u1; ++u) {
+    f4 w[4], d[FQ];
+    load(u, false, w, d);
+    multiply(w, d);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) parts[wave][k * FQ + j][lane] = acc[k][j];
+  __syncthreads();
+  if (wave > 0) return;
+  for (int o = 1; o < kFewWaves; ++o)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[k][j] += parts[o][k * FQ + j][lane];
+#pragma unroll
+  for (int j = 0; j < FQ; ++j) {
+    const int n = 16 * j + i;
+    if (n >= a.n) continue;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int p = c0 + 16 * g + 4 * r;
+      const f4 v = {acc[0][j][r], acc[1][j][r], acc[2][j][r], acc[3][j][r]};
+      if constexpr (EPI == kPartial) {
+        if (p < a.cols) *reinterpret_cast<f4*>(a.part + ((long long)split * a.n + n) * a.ldpart + p) = v;
+      } else {
+        f4 v1[1] = {v};
+        emit_linear<float, 1>(e, a.cols, a.n, n, 1, p, v1, f4{0.f, 0.f, 0.f, 0.f});
+      }
+    }
+  }
+}
+
 }  // namespace dense
 }  // namespace qcnn

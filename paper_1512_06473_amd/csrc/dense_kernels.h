@@ -700,6 +700,45 @@ Prod dx_prod(const Source<T>& w, const char* wp, int wrows, const char* dz, long
   return a;
 }
 
+// An input gradient's cut: of at most 32 rows in fp32, that of their own kernel
+// (splits and ldpart; steps: 16 rows each, of a wave).
+template <typename T>
+constexpr int kThinRows = sizeof(T) == 4 ? 32 : 0;
+
+template <typename T>
+Cut dx_cut(int cols, int N, int rows) {
+  if (N > kThinRows<T>) return cut_of<T>(cols, N, pad16<T>(rows), false);
+  Cut c = {};
+  const int groups = ceil_div(cols, 64), all = ceil_div(rows, 16);
+  c.splits = std::max(1, std::min(1024 / groups, all / (8 * kFewWaves)));
+  c.steps = ceil_div(all, kFewWaves * c.splits);
+  c.splits = ceil_div(all, kFewWaves * c.steps);
+  c.ldpart = (long long)ceil_div(cols, 4) * 4;
+  c.part_bytes = c.splits > 1 ? (size_t)c.splits * N * c.ldpart * 4 : 0;
+  return c;
+}
+
+// dx = dz w: d's columns are `stored`, whole dwords, `rows` without its zeros.
+template <typename T>
+hipError_t run_dx(const Source<T>& w, const char* wp, int rows, const char* d, long long ldd, int stored, int N,
+                  const Epi& e, const Cut& c, float* part, hipStream_t st) {
+  if constexpr (kThinRows<T> > 0) {
+    if (N <= kThinRows<T>) {
+      const Thin a = {reinterpret_cast<const float*>(wp), reinterpret_cast<const float*>(d), w.ld, ldd, rows, w.cols, N,
+                      c.steps, c.splits, part, c.ldpart};
+      const dim3 grid((unsigned)(ceil_div(w.cols, 64) * c.splits)), block(64 * kFewWaves);
+      auto launch = [&](auto kernel) {
+        LaunchTimer timer;
+        return timed_launch(&timer, kernel, grid, block, 0u, st, a, e);
+      };
+      if (c.splits == 1) return N <= 16 ? launch(thin_kernel<1, kLinear>) : launch(thin_kernel<2, kLinear>);
+      const hipError_t err = N <= 16 ? launch(thin_kernel<1, kPartial>) : launch(thin_kernel<2, kPartial>);
+      return err != hipSuccess ? err : finish<T, kLinear>(w.cols, N, e, c, part, st);
+    }
+  }
+  return run_product<T, true, false, kLinear, false>(dx_prod(w, wp, rows, d, ldd, stored, N), e, c, part, st);
+}
+
 // dw = dz^T x
 template <typename T>
 Prod dw_prod(const Source<T>& x, const char* dz, long long lddz, int stored, int wrows) {
@@ -740,7 +779,7 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
   const int rows = GATED ? 2 * s.Ct : s.Ct;
   Layout l;
   // With no activation dy is dz, where the products can read it in place.
-  const Cut cx = cut_of<T>(s.Cs, s.N, pad16<T>(rows), false), cw = cut_of<T>(s.Cs, rows, s.N, false);
+  const Cut cx = dx_cut<T>(s.Cs, s.N, rows), cw = cut_of<T>(s.Cs, rows, s.N, false);
   const bool fits = direct<T>(dy, s.ldy, s.Ct) && !(dx && ends_whole<T>(cx) && s.Ct * sizeof(T) % 16);
   const bool in_place = !GATED && act == QCNN_ACT_NONE && (fits || (!dx && !dw));
   const long long lddz = in_place ? s.ldy : pad16<T>(rows);
@@ -780,7 +819,7 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Epi p = {};
     p.y = dx;
     p.ldy = s.Cs;
-    e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr(), rows, dz, lddz, stored, s.N), p, cx, sums, st);
+    e = run_dx<T>(wsrc, wsrc.ptr(), rows, dz, lddz, stored, s.N, p, cx, sums, st);
     if (e != hipSuccess) return e;
   }
   if (dw) {
@@ -855,7 +894,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
   size_t part_bytes = 0;
   for (int n : {piece, s.Ct - (pieces - 1) * piece}) {
     part_bytes = std::max(part_bytes, Forward<T>(n, s.N, s.Cs, false).part_bytes);
-    if (dx) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, s.N, pad16<T>(n), false).part_bytes);
+    if (dx) part_bytes = std::max(part_bytes, dx_cut<T>(s.Cs, s.N, n).part_bytes);
     if (dw && !outer) part_bytes = std::max(part_bytes, cut_of<T>(s.Cs, n, s.N, false).part_bytes);
   }
   const size_t part = l.add(part_bytes);
@@ -909,8 +948,7 @@ hipError_t xent_backward(const LinearShape& s, const void* x, const void* w, con
       o.ldacc = ldacc;
       o.acc_in = k > 0;
       o.acc_out = k + 1 < pieces;
-      e = run_product<T, true, false, kLinear, false>(dx_prod(wsrc, wsrc.ptr() + c0 * wsrc.bytes(), n, d, ld, (int)ld, s.N), o,
-                                                      cut_of<T>(s.Cs, s.N, pad16<T>(n), false), sums, st);
+      e = run_dx<T>(wsrc, wsrc.ptr() + c0 * wsrc.bytes(), n, d, ld, (int)ld, s.N, o, dx_cut<T>(s.Cs, s.N, n), sums, st);
     }
     if (e == hipSuccess && dw) {
       Epi o = {};

@@ -569,3 +569,27 @@ def test_weight_gradients_of_few_rows(dev, tname, N, Cs, Ct):
     bound = product_bound(N, A, ref, T) + (2.0 ** -25 if T == torch.float16 else 0)
     near(flat[:Ct * Cs].view(Ct, Cs), ref, bound, "dw")
     assert (flat[Ct * Cs:] == 7).all()
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N", [1, 16, 17, 32, 33])
+@pytest.mark.parametrize("Cs,Ct", [(1, 1), (31, 127), (63, 4099), (333, 1025), (4100, 129), (70, 20000)])
+def test_input_gradients_of_few_rows(dev, tname, N, Cs, Ct):
+    """The same for dx, with NaN behind the last weight and the last dy."""
+    T = TYPES[tname]
+    wide_dy = torch.full((N, Ct + 5), float("nan"), dtype=T, device=dev)
+    flat_w = torch.full((Ct * Cs + 64,), float("nan"), dtype=T, device=dev)
+    dy, w = wide_dy[:, 3:3 + Ct], flat_w[:Ct * Cs].view(Ct, Cs)
+    dy.copy_(normal(dev, T, 1, N, Ct))
+    w.copy_(normal(dev, T, 2, Ct, Cs))
+    print("few rows dx", tname, N, Cs, Ct, flush=True)
+    flat = torch.full((N * Cs + 64,), 7.0, dtype=T, device=dev)
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[T]
+    rc = lib().qcnn_linear_backward(code, dy.data_ptr(), Ct + 5, None, 0, N, Cs, w.data_ptr(), Ct, None, 0,
+                                    flat.data_ptr(), None, None, None, None, torch.cuda.current_stream(dev).cuda_stream)
+    assert rc == 0
+    ref, A = torch.mm(dy.double(), w.double()), torch.mm(dy.double().abs(), w.double().abs())
+    # below 2^-14 fp16's numbers are 2^-24 apart: half a step is 2^-25, not 2^-11 of the value
+    bound = product_bound(Ct, A, ref, T) + (2.0 ** -25 if T == torch.float16 else 0)
+    near(flat[:N * Cs].view(N, Cs), ref, bound, "dx")
+    assert (flat[N * Cs:] == 7).all()
