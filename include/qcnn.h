@@ -433,7 +433,9 @@ qcnn_status qcnn_gated_backward(int dtype, const void* dy, long long lddy, const
  * sum per row.  labels [N] int64; a negative label leaves its row out (loss
  * and gradients 0, lse as usual); one >= C_t makes the row's loss and every
  * gradient that it enters NaN.  A bias of -infinity takes its class out (all
- * of them: NaN).  A row that is left out still has to be finite for dw. */
+ * of them: NaN).  A logit of NaN or +infinity, of whichever class, makes the
+ * row's loss (unless it is left out) and lse NaN.  A row that is left out
+ * still has to be finite for dw. */
 qcnn_status qcnn_linear_xent_forward(int dtype, const void* x, long long ldx, int N, int C_s, const void* w, int C_t,
                                      const void* bias, const int64_t* labels, float* loss, float* lse,
                                      void* workspace, size_t* workspace_bytes, void* stream);

@@ -341,12 +341,13 @@ __device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int nq, int q, 
   }
 }
 
-// (max, sum of exp(. - max)) of two disjoint sets.
+// (max, sum of exp(. - max)) of two disjoint sets.  fmaxf passes over NaN: the
+// sum is what carries it.  A set whose maximum is -inf is empty or masked and
+// has the sum 0, or NaN where a logit was that; either is added as it is.
 __device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
-  if (m == -INFINITY) return make_float2(m, a.y + b.y);  // both empty (sums 0)
-  const float sa = a.x == -INFINITY ? 0.f : a.y * __expf(a.x - m);
-  const float sb = b.x == -INFINITY ? 0.f : b.y * __expf(b.x - m);
+  const float sa = a.x == -INFINITY ? a.y : a.y * __expf(a.x - m);
+  const float sb = b.x == -INFINITY ? b.y : b.y * __expf(b.x - m);
   return make_float2(m, sa + sb);
 }
 

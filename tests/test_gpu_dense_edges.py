@@ -1,0 +1,127 @@
+"""The dense layers where numbers run out: NaN among a row's logits, loss
+weights and activations at the ends of their range, fp32's accuracy in one
+sign, and gradients of a size that a 16-bit type still holds.
+
+References are float64; tolerances count half steps of 2^-24 (fp32) or of the
+type, as in test_gpu_dense.py, and are derived at each test.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_1512_06473_amd import api
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+E32 = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+def normal(dev, T, seed, *shape, scale=1.0):
+    g = torch.Generator(device=dev).manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=dev) * scale).to(T)
+
+
+def near(got, want, bound, what):
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), what
+    over = float(((got.double() - want).abs() - bound).max())
+    assert over <= 0, "%s: over by %g" % (what, over)
+
+
+# N, C_s, C_t: few rows by 16 and by 32 columns a wave (fp32: 20 rows too);
+# small tiles; large ones and a tail; parts of k whose sums one workgroup a row
+# finishes, and several
+LOSSES = [(4, 64, 301), (13, 64, 16401), (20, 64, 301), (300, 64, 257), (1999, 136, 17001), (40, 4096, 257),
+          (70, 2048, 6001)]
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Cs,Ct", LOSSES)
+def test_nan_logits_reach_the_loss(dev, tname, N, Cs, Ct):
+    """Whichever class has them, and whatever its neighbours are: all of a
+    lane's, a quad's or a tile's classes NaN or masked, and others finite."""
+    T = TYPES[tname]
+    x, w = normal(dev, T, 1, N, Cs), normal(dev, T, 2, Ct, Cs, scale=1 / math.sqrt(Cs))
+    labels = torch.arange(N, device=dev) % 7 + 8  # no label is a class that is NaN or masked below
+    labels[1] = -1
+    counted = labels >= 0
+    nan, gone = float("nan"), float("-inf")
+    places = [0, 1, 2, 3, 4, 16, 17, 19, 64, 255, 256, Ct - 2, Ct - 1]
+    for c in places:
+        for masked in ((), (slice(max(0, c - c % 4), c), slice(c + 1, c + 4)), (slice(20, None),), (slice(1, 8),)):
+            bias = torch.zeros(Ct, dtype=T, device=dev)
+            for m in masked:
+                bias[m] = gone
+            bias[c] = nan
+            print("nan", tname, N, Cs, Ct, c, masked, flush=True)
+            loss, lse = api.linear_xent_forward(x, w, labels, bias)
+            assert torch.isnan(lse).all() and torch.isnan(loss[counted]).all() and loss[1] == 0, (c, masked)
+    for rows in (slice(0, 1), slice(3, 4), slice(Ct - 1, Ct), slice(16, min(Ct, 16 + 512)), slice(Ct - 200, Ct)):
+        bad = w.clone()
+        bad[rows] = nan
+        loss, lse = api.linear_xent_forward(x, bad, labels)
+        assert torch.isnan(lse).all() and torch.isnan(loss[counted]).all() and loss[1] == 0, rows
+    dx, dw, db = api.linear_xent_backward(torch.full((N,), 1.0 / N, device=dev), lse, x, w, labels, need_dbias=True)
+    assert torch.isnan(dx[counted]).all() and (dx[1] == 0).all() and torch.isnan(dw).all() and torch.isnan(db).all()
+    bias = torch.zeros(Ct, dtype=T, device=dev)
+    bias[Ct - 1] = float("inf")  # inf - inf
+    loss, lse = api.linear_xent_forward(x, w, labels, bias)
+    assert torch.isnan(lse).all() and torch.isnan(loss[counted]).all() and loss[1] == 0
+    # a row of x: that row alone
+    x[2, 3] = nan
+    loss, lse = api.linear_xent_forward(x, w, labels)
+    keep = torch.arange(N, device=dev) != 2
+    assert torch.isnan(lse[2]) and torch.isnan(loss[2])
+    assert torch.isfinite(lse[keep]).all() and torch.isfinite(loss[keep]).all()
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Cs,Ct", LOSSES)
+def test_classes_masked_all_but_one(dev, tname, N, Cs, Ct):
+    """The joins of empty sets with the one that is left: its logit is lse."""
+    T = TYPES[tname]
+    x, w = normal(dev, T, 1, N, Cs), normal(dev, T, 2, Ct, Cs, scale=1 / math.sqrt(Cs))
+    for c in (0, 3, 130, Ct - 1):
+        bias = torch.full((Ct,), float("-inf"), dtype=T, device=dev)
+        bias[c] = 0
+        loss, lse = api.linear_xent_forward(x, w, torch.full((N,), c, device=dev), bias)
+        z = torch.mm(x.double(), w[c:c + 1].double().t())[:, 0]
+        # a sum of C_s products, then log(1) = 0 is added
+        A = torch.mm(x.double().abs(), w[c:c + 1].double().abs().t())[:, 0]
+        near(lse, z, 8 * math.sqrt(Cs) * E32 * A + 2 * E32 * z.abs(), "lse")
+        assert (loss == 0).all()
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N", [4, 200])
+def test_nan_and_infinities_in_the_gated_layer(dev, tname, N):
+    """They go where the formula takes them and nowhere else."""
+    T = TYPES[tname]
+    x, w = normal(dev, T, 1, N, 96), normal(dev, T, 2, 2 * 75, 96, scale=0.1)
+    z, A = torch.mm(x.double(), w.double().t()), torch.mm(x.double().abs(), w.double().abs().t())
+    gate, up = z[:, :75] * torch.sigmoid(z[:, :75]), z[:, 75:]
+    want, e = gate * up, 8 * math.sqrt(96) * E32 * A
+    # each factor's error times the other factor, silu's slope at most 1.1; one rounding (fp16: or half of 2^-24)
+    bound = 1.1 * e[:, :75] * (up.abs() + e[:, 75:]) + e[:, 75:] * gate.abs() + 16 * E32 * z[:, :75].abs() * up.abs() + \
+        torch.finfo(T).eps / 2 * want.abs() + (2.0 ** -25 if T == torch.float16 else 0)
+    x[2, 5] = float("nan")
+    x[3, 7] = float("inf")
+    w2 = w.clone()
+    w2[10, 1], w2[75 + 20, 2] = float("nan"), float("inf")
+    keep = [n for n in range(N) if n not in (2, 3)]
+    y = api.gated_forward(x, w)
+    assert torch.isnan(y[2]).all() and not torch.isfinite(y[3]).any()
+    near(y[keep], want[keep], bound[keep], "rows")
+    y = api.gated_forward(x, w2)
+    assert torch.isnan(y[:, 10]).all() and not torch.isfinite(y[:, 20]).any()
+    cols = [c for c in range(75) if c not in (10, 20)]
+    near(y[keep][:, cols], want[keep][:, cols], bound[keep][:, cols], "columns")
