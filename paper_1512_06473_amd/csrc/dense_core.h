@@ -161,7 +161,7 @@ struct Epi {
   const long long* labels;
   const float* lse;
   const float* dloss;
-  const float* dmax;  // device scalar: the largest |dloss| (1 where that is 0)
+  const float* dmax;  // device scalar: dmax_kernel's out[0]
   float gain;
   float2* stat;       // [slot][nq]: maximum and sum of exponentials of a slot's logits
   float* zlabel;      // [nq]: the label's logit

@@ -324,7 +324,8 @@ static __global__ __launch_bounds__(THREADS) void loss_kernel(const float2* __re
 }
 
 // out[0] = the largest finite |dloss| of a counted row (1 if there is none or
-// it is 0), out[1] = out[0] / gain: what products with d are multiplied by.
+// it is 0; 2^-110 at least, so that gain / out[0] is finite and out[1] a normal
+// number), out[1] = out[0] / gain: what products with d are multiplied by.
 static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restrict__ dloss,
                                                     const long long* __restrict__ labels, int n, float gain,
                                                     float* __restrict__ out) {
@@ -340,7 +341,7 @@ static __global__ __launch_bounds__(1024) void dmax_kernel(const float* __restri
   __syncthreads();
   if (threadIdx.x) return;
   for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i]);
-  if (m == 0.f) m = 1.f;
+  m = m == 0.f ? 1.f : fmaxf(m, 0x1p-110f);
   out[0] = m;
   out[1] = m / gain;
 }

@@ -125,3 +125,42 @@ def test_nan_and_infinities_in_the_gated_layer(dev, tname, N):
     assert torch.isnan(y[:, 10]).all() and not torch.isfinite(y[:, 20]).any()
     cols = [c for c in range(75) if c not in (10, 20)]
     near(y[keep][:, cols], want[keep][:, cols], bound[keep][:, cols], "columns")
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N", [6, 150])
+@pytest.mark.parametrize("c", [2.0 ** -100, 2.0 ** -119, 2.0 ** -127, 2.0 ** -140])
+def test_smallest_loss_weights(dev, tname, N, c):
+    """Weights whose reciprocal no float holds, beside rows of weight 0 and
+    rows left out.  Large x (small w: logits of ordinary size) bring dw back
+    into fp32's and bf16's normal range; all of fp16's gradients round to 0."""
+    T = TYPES[tname]
+    up = 1.0 if T == torch.float16 else 2.0 ** 60
+    Cs, Ct = 64, 90
+    x, w = normal(dev, T, 1, N, Cs, scale=up), normal(dev, T, 2, Ct, Cs, scale=1 / (8 * up))
+    labels = torch.arange(N, device=dev) % Ct
+    labels[4] = -1
+    weight = torch.full((N,), c, device=dev)
+    weight[1::2] = 0.0
+    _, lse = api.linear_xent_forward(x, w, labels)
+    dx, dw, db = api.linear_xent_backward(weight, lse, x, w, labels, need_dbias=True)
+    for g in (dx, dw, db):
+        assert torch.isfinite(g).all()
+    if T == torch.float16:
+        assert (dx == 0).all() and (dw == 0).all() and (db == 0).all()
+        return
+    z = torch.mm(x.double(), w.double().t())
+    p = torch.softmax(z, 1)
+    d = p.clone()
+    d[torch.arange(N, device=dev), labels.clamp(min=0)] -= 1.0
+    on = torch.where(labels >= 0, weight.double(), torch.zeros(N, dtype=torch.float64, device=dev))[:, None]
+    d = d * on
+    # a logit is off by its sum's rounding, lse too, and exp passes that on; d is rounded to T once
+    ez = 8 * math.sqrt(Cs) * E32 * torch.mm(x.double().abs(), w.double().abs().t()).max(1).values[:, None] + 64 * E32
+    off = torch.finfo(T).eps / 2 * d.abs() + on * (2 * ez * p + 8 * E32)
+    ref, A = torch.mm(d.t(), x.double()), torch.mm(d.t().abs(), x.double().abs())
+    near(dw, ref, (8 * math.sqrt(N) + 4) * E32 * A + torch.finfo(T).eps / 2 * ref.abs() + torch.mm(off.t(), x.double().abs()),
+         "dw")
+    # what is left of dbias and dx is subnormal or 0: within one smallest normal number
+    near(db, d.sum(0), off.sum(0) + 2 * torch.finfo(T).eps * d.abs().sum(0) + 2.0 ** -126, "dbias")
+    near(dx, torch.mm(d, w.double()), torch.full((N, Cs), 2.0 ** -126, dtype=torch.float64, device=dev), "dx")
