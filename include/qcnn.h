@@ -370,7 +370,8 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
  * with whole 16 bytes, x and w are first copied into the workspace.  Forward
  * calls of few rows copy nothing.
  * Overlap: the range from an output's first element to its last, what lies
- * between its rows included, meets no other argument's range (QCNN_ERR_ALIAS).
+ * between its rows included, meets no other argument's range; nor does the
+ * caller's workspace (QCNN_ERR_ALIAS).
  * Limits: N <= 2^21; C_s, C_t (2 C_t of the gated layer) and strides <= 2^20;
  * no more than 2^22 tiles of 128 x 128 in any of the products
  * (QCNN_ERR_UNSUPPORTED past them).  Sizes are at least 1.

@@ -19,8 +19,11 @@ struct Span {
 
 bool meet(const Span& a, const Span& b) {
   const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-  return a.p && b.p && a0 < b0 + b.bytes && b0 < a0 + a.bytes;
+  return a.p && b.p && (a0 <= b0 ? b0 - a0 < a.bytes : a0 - b0 < b.bytes);  // no sum that could wrap
 }
+
+// The caller's workspace, which is written as outputs are.
+Span room(const void* workspace, const size_t* bytes) { return {workspace, workspace && bytes ? *bytes : 0}; }
 
 // An output overlaps an input or another output.
 bool aliased(std::initializer_list<Span> in, std::initializer_list<Span> out) {
@@ -86,8 +89,8 @@ qcnn_status backward(bool gated, int dtype, const void* dy, long long lddy, cons
   if (st != QCNN_OK) return st;
   const size_t rows = (size_t)halves * C_t, nw = rows * C_s * s, nx = (size_t)N * C_s * s;
   if (aliased({{dy, span(N, lddy, C_t, s)}, {dw ? x : nullptr, span(N, ldx, C_s, s)}, {dx ? w : nullptr, nw},
-               {pre, rows * N * s}, {workspace, workspace && workspace_bytes ? *workspace_bytes : 0}},
-              {{dx, nx}, {dw, nw}, {dbias, rows * s}}))
+               {pre, rows * N * s}},
+              {{dx, nx}, {dw, nw}, {dbias, rows * s}, room(workspace, workspace_bytes)}))
     return QCNN_ERR_ALIAS;
   DenseCall c = {};
   c.op = gated ? qcnn::dense::kGatedBackward : qcnn::dense::kLinearBackward;
@@ -117,8 +120,8 @@ qcnn_status qcnn_linear_forward(int dtype, const void* x, long long ldx, int N, 
                                {x, w, bias, residual, pre, y});
   if (st != QCNN_OK) return st;
   if (aliased({{x, span(N, ldx, C_s, s)}, {w, (size_t)C_t * C_s * s}, {bias, (size_t)C_t * s},
-               {residual, span(N, ldr, C_t, s)}, {workspace, workspace && workspace_bytes ? *workspace_bytes : 0}},
-              {{y, span(N, ldy, C_t, s)}, {pre, (size_t)N * C_t * s}}))
+               {residual, span(N, ldr, C_t, s)}},
+              {{y, span(N, ldy, C_t, s)}, {pre, (size_t)N * C_t * s}, room(workspace, workspace_bytes)}))
     return QCNN_ERR_ALIAS;
   DenseCall c = {};
   c.op = qcnn::dense::kLinearForward;
@@ -148,9 +151,8 @@ qcnn_status qcnn_gated_forward(int dtype, const void* x, long long ldx, int N, i
   const qcnn_status st = check(dtype, act, N, C_s, C_t, 2, {ldx, C_s, ldy, C_t}, {x, w, bias, pre, y});
   if (st != QCNN_OK) return st;
   const size_t rows = 2 * (size_t)C_t;
-  if (aliased({{x, span(N, ldx, C_s, s)}, {w, rows * C_s * s}, {bias, rows * s},
-               {workspace, workspace && workspace_bytes ? *workspace_bytes : 0}},
-              {{y, span(N, ldy, C_t, s)}, {pre, N * rows * s}}))
+  if (aliased({{x, span(N, ldx, C_s, s)}, {w, rows * C_s * s}, {bias, rows * s}},
+              {{y, span(N, ldy, C_t, s)}, {pre, N * rows * s}, room(workspace, workspace_bytes)}))
     return QCNN_ERR_ALIAS;
   DenseCall c = {};
   c.op = qcnn::dense::kGatedForward;
@@ -179,9 +181,8 @@ qcnn_status qcnn_linear_xent_forward(int dtype, const void* x, long long ldx, in
   const qcnn_status st = check(dtype, QCNN_ACT_NONE, N, C_s, C_t, 1, {ldx, C_s}, {x, w, bias});
   if (st != QCNN_OK) return st;
   if (((uintptr_t)labels & 7) || (((uintptr_t)loss | (uintptr_t)lse) & 3)) return QCNN_ERR_UNSUPPORTED;
-  if (aliased({{x, span(N, ldx, C_s, s)}, {w, (size_t)C_t * C_s * s}, {bias, (size_t)C_t * s}, {labels, (size_t)N * 8},
-               {workspace, workspace && workspace_bytes ? *workspace_bytes : 0}},
-              {{loss, (size_t)N * 4}, {lse, (size_t)N * 4}}))
+  if (aliased({{x, span(N, ldx, C_s, s)}, {w, (size_t)C_t * C_s * s}, {bias, (size_t)C_t * s}, {labels, (size_t)N * 8}},
+              {{loss, (size_t)N * 4}, {lse, (size_t)N * 4}, room(workspace, workspace_bytes)}))
     return QCNN_ERR_ALIAS;
   DenseCall c = {};
   c.op = qcnn::dense::kXentForward;
@@ -206,9 +207,8 @@ qcnn_status qcnn_linear_xent_backward(int dtype, const float* dloss, const float
   if (((uintptr_t)labels & 7) || (((uintptr_t)dloss | (uintptr_t)lse) & 3)) return QCNN_ERR_UNSUPPORTED;
   const size_t nw = (size_t)C_t * C_s * s;
   if (aliased({{x, span(N, ldx, C_s, s)}, {w, nw}, {bias, (size_t)C_t * s}, {labels, (size_t)N * 8},
-               {dloss, (size_t)N * 4}, {lse, (size_t)N * 4},
-               {workspace, workspace && workspace_bytes ? *workspace_bytes : 0}},
-              {{dx, (size_t)N * C_s * s}, {dw, nw}, {dbias, (size_t)C_t * s}}))
+               {dloss, (size_t)N * 4}, {lse, (size_t)N * 4}},
+              {{dx, (size_t)N * C_s * s}, {dw, nw}, {dbias, (size_t)C_t * s}, room(workspace, workspace_bytes)}))
     return QCNN_ERR_ALIAS;
   DenseCall c = {};
   c.op = qcnn::dense::kXentBackward;

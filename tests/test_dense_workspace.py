@@ -1,0 +1,48 @@
+"""Workspaces of the dense layers' C ABI, without a GPU: what may not overlap
+them, and how large they are.  The checks and the size query come before any
+HIP call (the device pointers are made up and never followed)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_1512_06473_amd import _lib, quantize_net
+
+ALIAS, WORKSPACE = 7, 8
+F32, BF16, F16 = 0, 1, 2
+
+
+def at(n):
+    return n << 36  # arrays 64 GiB apart
+
+
+@pytest.fixture(scope="module")
+def L():
+    return _lib.lib()
+
+
+LINEAR = dict(dtype=BF16, x=at(1), ldx=64, N=40, Cs=64, w=at(2), Ct=32, bias=at(3), act=4, residual=at(4), ldr=32,
+              pre=at(5), y=at(6), ldy=32)
+GRAD = dict(dtype=BF16, dy=at(1), lddy=32, x=at(2), ldx=64, N=40, Cs=64, w=at(3), Ct=32, pre=at(4), act=2, dx=at(5),
+            dw=at(6), dbias=at(7))
+GATED = dict(dtype=F16, x=at(1), ldx=64, N=40, Cs=64, w=at(2), Ct=32, bias=at(3), act=4, pre=at(5), y=at(6), ldy=32)
+XENT = dict(dtype=F32, x=at(1), ldx=64, N=40, Cs=64, w=at(2), Ct=32, bias=at(3), labels=at(4), loss=at(5), lse=at(6))
+XGRAD = dict(dtype=F32, dloss=at(8), lse=at(6), x=at(1), ldx=64, N=40, Cs=64, w=at(2), Ct=32, bias=at(3),
+             labels=at(4), dx=at(9), dw=at(10), dbias=at(11))
+CALLS = {"qcnn_linear_forward": LINEAR, "qcnn_linear_backward": GRAD, "qcnn_gated_forward": GATED,
+         "qcnn_gated_backward": GRAD, "qcnn_linear_xent_forward": XENT, "qcnn_linear_xent_backward": XGRAD}
+
+
+@pytest.mark.parametrize("entry,name", [(e, k) for e, args in CALLS.items() for k, v in args.items() if v >= at(1)])
+def test_a_workspace_overlaps_no_argument(L, entry, name):
+    """It is written like an output: no input, not even its last byte, may lie in it."""
+    f, args = getattr(L, entry), CALLS[entry]
+    size = ctypes.c_size_t(1 << 20)
+    assert f(*args.values(), args[name], ctypes.byref(size), None) == ALIAS          # on it
+    assert f(*args.values(), args[name] - (1 << 19), ctypes.byref(size), None) == ALIAS  # reaching into it
+    size = ctypes.c_size_t(2 ** 64 - 1)                                               # as long as can be said
+    assert f(*args.values(), args[name] - (1 << 19), ctypes.byref(size), None) == ALIAS
+    # right in front of it: past the check, and refused as too small before anything is launched
+    size = ctypes.c_size_t(256)
+    args = dict(args, Cs=65, ldx=65, N=200)  # larger than the caller's 256 bytes
+    assert f(*args.values(), args[name] - 256, ctypes.byref(size), None) == WORKSPACE
