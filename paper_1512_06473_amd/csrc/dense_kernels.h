@@ -114,9 +114,11 @@ __global__ __launch_bounds__(256) void slope_kernel(const Slope a) {
         s0[k] += g[k];
         s1[k] += u[k];
       }
-      T* o = static_cast<T*>(a.dz) + r * a.lddz + p;
-      store_wide(o, n, g);
-      store_wide(o + a.cols, n, u);
+      if (a.dz) {
+        T* o = static_cast<T*>(a.dz) + r * a.lddz + p;
+        store_wide(o, n, g);
+        store_wide(o + a.cols, n, u);
+      }
     } else {
       if (a.act != QCNN_ACT_NONE) {
         load_wide(static_cast<const T*>(a.pre) + r * a.ldpre + p, n, g);
@@ -779,17 +781,21 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
                           void* dx, void* dw, void* dbias, const Room& room, hipStream_t st) {
   const int rows = GATED ? 2 * s.Ct : s.Ct;
   Layout l;
-  // With no activation dy is dz, where the products can read it in place.
+  // With no activation dy is dz, where the products can read it in place; with
+  // no products dz is only summed.
+  const bool products = dx || dw;
   const Cut cx = dx_cut<T>(s.Cs, s.N, rows), cw = cut_of<T>(s.Cs, rows, s.N, false);
   const bool fits = direct<T>(dy, s.ldy, s.Ct) && !(dx && ends_whole<T>(cx) && s.Ct * sizeof(T) % 16);
-  const bool in_place = !GATED && act == QCNN_ACT_NONE && (fits || (!dx && !dw));
+  const bool in_place = !GATED && act == QCNN_ACT_NONE && (fits || !products);
   const long long lddz = in_place ? s.ldy : pad16<T>(rows);
   const int stored = in_place ? rows : pad16<T>(rows);
-  const size_t dz_at = in_place ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
+  const bool kept = products && !in_place;
+  const size_t dz_at = !kept ? 0 : l.add((size_t)s.N * lddz * sizeof(T));
   const int chunk = slope_chunk(s.N), chunks = ceil_div(s.N, chunk);
   const size_t sums_at = dbias ? l.add((size_t)chunks * rows * 4) : 0;
   const bool outer = few_outer(s.N);
-  Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l, !outer), wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l);
+  Source<T> xs(dw ? x : nullptr, dw ? s.ldx : 0, s.N, s.Cs, &l, dw && !outer),
+      wsrc(dx ? w : nullptr, s.Cs, rows, s.Cs, &l, dx != nullptr);
   const size_t part = l.add(std::max(dx ? cx.part_bytes : 0, dw && !outer ? cw.part_bytes : 0));
   Scratch ws;
   bool asked;
@@ -803,7 +809,7 @@ hipError_t layer_backward(const LinearShape& s, const void* dy, const void* x, c
     Slope a = {};
     a.dy = dy;
     a.pre = pre;
-    a.dz = in_place ? nullptr : ws.get() + dz_at;
+    a.dz = kept ? ws.get() + dz_at : nullptr;
     a.part = dbias ? reinterpret_cast<float*>(ws.get() + sums_at) : nullptr;
     a.lddy = s.ldy;
     a.ldpre = rows;

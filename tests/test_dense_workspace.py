@@ -46,3 +46,26 @@ def test_a_workspace_overlaps_no_argument(L, entry, name):
     size = ctypes.c_size_t(256)
     args = dict(args, Cs=65, ldx=65, N=200)  # larger than the caller's 256 bytes
     assert f(*args.values(), args[name] - 256, ctypes.byref(size), None) == WORKSPACE
+
+
+def need(L, entry, args):
+    n = ctypes.c_size_t(0)
+    assert getattr(L, entry)(*args.values(), None, ctypes.byref(n), None) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("entry,halves", [("qcnn_linear_backward", 1), ("qcnn_gated_backward", 2)])
+@pytest.mark.parametrize("act", [0, 2])
+@pytest.mark.parametrize("Cs", [4096, 4095])
+def test_nothing_is_reserved_for_what_is_not_read(L, entry, halves, act, Cs):
+    """4095 columns of a 16-bit type are copied to rows of 4096: of x for dw
+    only, of w for dx only.  dbias alone needs its sums, no dz."""
+    N, rows = 4096, halves * 4096
+    full = dict(GRAD, N=N, Cs=Cs, ldx=Cs, Ct=4096, lddy=4096, act=act)
+    full = {k: v << 2 if v >= at(1) else v for k, v in full.items()}
+    whole = need(L, entry, full)
+    dbias = need(L, entry, dict(full, dx=None, dw=None, x=None, w=None))
+    assert dbias <= 512 * rows * 4 + 256
+    copies = (2 * 4096 * N, 2 * 4096 * rows) if Cs % 2 else (0, 0)
+    assert need(L, entry, dict(full, dx=None, w=None)) <= whole - copies[1]
+    assert need(L, entry, dict(full, dw=None, x=None)) <= whole - copies[0]

@@ -164,3 +164,18 @@ def test_smallest_loss_weights(dev, tname, N, c):
     # what is left of dbias and dx is subnormal or 0: within one smallest normal number
     near(db, d.sum(0), off.sum(0) + 2 * torch.finfo(T).eps * d.abs().sum(0) + 2.0 ** -126, "dbias")
     near(dx, torch.mm(d, w.double()), torch.full((N, Cs), 2.0 ** -126, dtype=torch.float64, device=dev), "dx")
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Ct", [(1, 1), (11, 77), (32, 1000), (33, 513), (700, 130)])
+def test_bias_gradients_alone(dev, tname, N, Ct):
+    """The same bits as beside the products."""
+    T = TYPES[tname]
+    x, w, dy, pre = (normal(dev, T, k, *s) for k, s in enumerate([(N, 65), (2 * Ct, 65), (N, Ct), (N, 2 * Ct)]))
+    for act in ("none", "relu", "gelu", "gelu_tanh", "silu"):
+        alone = api.gated_backward(dy, x, w, pre, act=act, need_dx=False, need_dw=False)
+        assert alone[0] is None and alone[1] is None
+        assert torch.equal(alone[2], api.gated_backward(dy, x, w, pre, act=act)[2])
+        half = pre[:, :Ct].contiguous()
+        alone = api.linear_backward(dy, x, w[:Ct], act=act, pre=half, need_dx=False, need_dw=False)
+        assert torch.equal(alone[2], api.linear_backward(dy, x, w[:Ct], act=act, pre=half)[2])
