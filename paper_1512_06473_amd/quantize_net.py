@@ -35,9 +35,11 @@ def fc_responses(x: torch.Tensor, specs: List[dict]) -> List[torch.Tensor]:
         raise ValueError("fc_responses takes fully-connected layers only")
     h = x.reshape(x.shape[0], -1).contiguous()
     out: List[torch.Tensor] = []
-    for spec in specs:
+    for k, spec in enumerate(specs):
         W, bias, act = spec["W"], spec.get("bias"), "relu" if spec["relu"] else "none"
-        if bias is None:  # the response is what the activation sees
+        if k + 1 == len(specs):  # no layer reads its output
+            T = api.linear_forward(h, W)
+        elif bias is None:  # the response is what the activation sees
             T = torch.empty((h.shape[0], W.shape[0]), dtype=torch.float32, device=h.device)
             h = api.linear_forward(h, W, act=act, pre=T)
         else:

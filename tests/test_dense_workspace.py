@@ -69,3 +69,32 @@ def test_nothing_is_reserved_for_what_is_not_read(L, entry, halves, act, Cs):
     copies = (2 * 4096 * N, 2 * 4096 * rows) if Cs % 2 else (0, 0)
     assert need(L, entry, dict(full, dx=None, w=None)) <= whole - copies[1]
     assert need(L, entry, dict(full, dw=None, x=None)) <= whole - copies[0]
+
+
+def test_responses_take_no_product_that_nobody_reads(monkeypatch):
+    """One product per layer without a bias; two with one (the response has
+    none), but for the last layer, whose output no layer reads."""
+    calls = []
+
+    def linear(x, w, bias=None, act="none", residual=None, out=None, pre=None):
+        z = x @ w.t()
+        if pre is not None:
+            pre.copy_(z if bias is None else z + bias)
+        calls.append((tuple(w.shape), act))
+        z = z if bias is None else z + bias
+        return torch.relu(z) if act == "relu" else z
+
+    monkeypatch.setattr(quantize_net.api, "linear_forward", linear)
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(5, 2, 4, generator=g)
+    for biased in (True, False):
+        calls.clear()
+        specs = [{"kind": "fc", "W": torch.randn(ct, cs, generator=g), "relu": True,
+                  "bias": torch.randn(ct, generator=g) if biased else None} for cs, ct in ((8, 6), (6, 7), (7, 3))]
+        got, h = quantize_net.fc_responses(x, specs), x.reshape(5, 8)
+        for t, s in zip(got, specs):
+            z = h @ s["W"].t()
+            assert torch.equal(t, z)
+            h = torch.relu(z + s["bias"] if biased else z)
+        assert len(calls) == (5 if biased else 3)
+    assert quantize_net.fc_responses(x, []) == []
