@@ -33,7 +33,9 @@
 namespace qcnn {
 namespace dense {
 
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
@@ -439,19 +441,23 @@ struct Operand {
   }
 };
 
-// Four fp32 values as three bf16 parts each: the upper 8 bits of the 24, the
-// next 8, the last 8, each cut off (not rounded, so that nothing overflows),
-// which is exact.  Of the nine products of two numbers' parts the three
-// smallest, below 2^-22 of the whole, are left out.
+// Four fp32 values as three bf16 parts each: the nearest 8 bits of the 24, the
+// nearest 8 of what is left, and the rest, which is exact.  Of the nine products
+// of two numbers' parts the three smallest are left out: the parts are at most
+// 2^-8 and 2^-17 of a number in [1, 2), so these come to 2^-24 of the product,
+// of either sign (upper bits cut off: 2^-21, always shrinking it).  The largest
+// numbers round to an infinity; their tiles are computed again.
 __device__ __forceinline__ void split_bf16(f4 x, uint2 (&out)[3]) {
 #pragma unroll
   for (int n = 0; n < 3; ++n) {
-    uint32_t u[4];
+    uint32_t u[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(x[i]);
-    out[n] = make_uint2(__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] -= __uint_as_float(u[i] & 0xffff0000u);
+    for (int i = 0; i < 2; ++i) {
+      u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x[2 * i], x[2 * i + 1]}, b2));
+      x[2 * i] -= __uint_as_float(u[i] << 16);
+      x[2 * i + 1] -= __uint_as_float(u[i] & 0xffff0000u);
+    }
+    out[n] = make_uint2(u[0], u[1]);
   }
 }
 

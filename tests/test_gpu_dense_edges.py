@@ -179,3 +179,44 @@ def test_bias_gradients_alone(dev, tname, N, Ct):
         half = pre[:, :Ct].contiguous()
         alone = api.linear_backward(dy, x, w[:Ct], act=act, pre=half, need_dx=False, need_dw=False)
         assert torch.equal(alone[2], api.linear_backward(dy, x, w[:Ct], act=act, pre=half)[2])
+
+
+@pytest.mark.parametrize("n", [1, 2, 4])
+def test_fp32_products_of_one_sign(dev, n):
+    """Numbers just below 1 + 2^-7: were their upper 8 bits cut off, 16 bits of
+    each would be left, and the smallest products of the parts, which are left
+    out, would come to 8 x 2^-24 of a product, always of one sign.  Rounded to
+    the nearest 8 bits they are 1 + 2^-7 less 2^-23, with nothing left out.  Of
+    n = 1, 2 or 4 equal products every partial sum up to the last addition is
+    exact or below 2^-21 of the whole: off by half a step at the end, 2^-24, or
+    a whole one if the matrix cores cut off, and 2^-44: within 3 x 2^-24."""
+    v = 1 + 2.0 ** -7 - 2.0 ** -23
+    N, C = 70, 130
+    for sign in (1.0, -1.0):
+        x, w = torch.zeros(N, C, device=dev), torch.zeros(150, C, device=dev)
+        x[:, :n], w[:, :n] = v, sign * v
+        want = torch.full((N, 150), n * sign * v * v, dtype=torch.float64, device=dev)
+        near(api.linear_forward(x, w), want, 3 * E32 * want.abs(), "y")
+        dy, w = torch.zeros(N, 150, device=dev), torch.full((150, C), v, device=dev)
+        dy[:, 100:100 + n] = sign * v
+        dx, _, _ = api.linear_backward(dy, x, w, need_dw=False)
+        want = torch.full((N, C), n * sign * v * v, dtype=torch.float64, device=dev)
+        near(dx, want, 3 * E32 * want.abs(), "dx")
+        dy, x = torch.zeros(N, 150, device=dev), torch.full((N, C), v, device=dev)
+        dy[60:60 + n] = sign * v
+        _, dw, _ = api.linear_backward(dy, x, w, need_dx=False)
+        want = torch.full((150, C), n * sign * v * v, dtype=torch.float64, device=dev)
+        near(dw, want, 3 * E32 * want.abs(), "dw")
+
+
+def test_fp32_largest_numbers(dev):
+    """Up to the largest there is, whose upper bits round to an infinity: as
+    exact as any other, in ordinary sums."""
+    top = torch.finfo(torch.float32).max
+    for N in (8, 70):
+        x, w = normal(dev, torch.float32, 1, N, 40), normal(dev, torch.float32, 2, 150, 40, scale=2.0 ** -6)
+        x[1, 3], x[2, 4] = top, -top
+        w[:, 3:5] *= 2.0 ** -4
+        y, ref = api.linear_forward(x, w), torch.mm(x.double(), w.double().t())
+        A = torch.mm(x.double().abs(), w.double().abs().t())
+        near(y, ref, 8 * math.sqrt(40) * E32 * A + E32 * ref.abs(), "%d rows" % N)
