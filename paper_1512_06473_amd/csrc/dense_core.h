@@ -63,8 +63,9 @@ struct Num<float> {
   }
   static __device__ __forceinline__ float exp_(float x) { return expf(x); }
   static __device__ __forceinline__ float div_(float a, float b) { return a / b; }
-  // The normal distribution function; density = exp(-z^2 / 2).
-  static __device__ __forceinline__ float phi(float z, float) { return 0.5f * (1.f + erff(z * 0.70710678118654752f)); }
+  // The normal distribution function; density = exp(-z^2 / 2).  By erfc, which
+  // keeps its digits where 1 + erf cancels (below z = -5.5 nothing is left of it).
+  static __device__ __forceinline__ float phi(float z, float) { return 0.5f * erfcf(z * -0.70710678118654752f); }
 };
 
 // 16-bit results carry 8 or 11 bits: the hardware's exponential and reciprocal

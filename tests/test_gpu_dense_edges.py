@@ -220,3 +220,20 @@ def test_fp32_largest_numbers(dev):
         y, ref = api.linear_forward(x, w), torch.mm(x.double(), w.double().t())
         A = torch.mm(x.double().abs(), w.double().abs().t())
         near(y, ref, 8 * math.sqrt(40) * E32 * A + E32 * ref.abs(), "%d rows" % N)
+
+
+@pytest.mark.parametrize("N", [8, 40])
+def test_gelu_of_negative_numbers_in_fp32(dev, N):
+    """Phi(z) far down its tail, to a few steps of itself (1 + erf would leave
+    nothing below -5.5).  z / sqrt(2) is off by 1.5 half steps, and the tail
+    passes on 1 + z^2 times that; the function itself is good to 16 steps."""
+    z = torch.linspace(-12.0, 6.0, 3001, device=dev)
+    zd = z.double()
+    phi = 0.5 * torch.special.erfc(-zd / math.sqrt(2.0))
+    steps = 1.5 * zd * zd + 48
+    y = api.linear_forward(torch.ones(N, 1, device=dev), z[:, None].contiguous(), act="gelu")
+    near(y, (zd * phi).expand(N, -1), (steps * E32 * (zd * phi).abs()).expand(N, -1), "gelu")
+    dx, _, _ = api.linear_backward(torch.ones(3001, 1, device=dev), z[:, None], torch.ones(1, 1, device=dev), act="gelu",
+                                   pre=z[:, None].contiguous(), need_dw=False, need_dbias=False)
+    density = torch.exp(-0.5 * zd * zd) / math.sqrt(2.0 * math.pi)
+    near(dx[:, 0], phi + zd * density, steps * E32 * (phi + (zd * density).abs()), "slope")
