@@ -135,7 +135,8 @@ __device__ __forceinline__ float act_slope(int act, float z) {
     }
     case QCNN_ACT_GELU_TANH: {
       const float s = Num<T>::div_(1.f, 1.f + Num<T>::exp_(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
-      return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * z * z);
+      // z^2 overflows from 2^64 on, where s (1 - s) is 0.
+      return s + z * s * (1.f - s) * 1.5957691216057308f * (1.f + 0.134145f * fminf(z * z, 0x1p100f));
     }
     case QCNN_ACT_SILU: {
       const float s = Num<T>::div_(1.f, 1.f + Num<T>::exp_(-z));

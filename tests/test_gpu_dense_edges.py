@@ -237,3 +237,23 @@ def test_gelu_of_negative_numbers_in_fp32(dev, N):
                                    pre=z[:, None].contiguous(), need_dw=False, need_dbias=False)
     density = torch.exp(-0.5 * zd * zd) / math.sqrt(2.0 * math.pi)
     near(dx[:, 0], phi + zd * density, steps * E32 * (phi + (zd * density).abs()), "slope")
+
+
+@pytest.mark.parametrize("tname", ["fp32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_activations_of_the_largest_numbers(dev, tname, act):
+    """From where z^2 overflows up to the largest number: z and 0, slopes 1 and 0."""
+    T = TYPES[tname]
+    z = torch.tensor([1e13, 1e18, 3e19, 1e20, 1e30, float(torch.finfo(T).max)], dtype=torch.float64).to(T).to(dev)
+    z = torch.cat([z, -z])[:, None].contiguous()
+    one, up = torch.ones(1, 1, dtype=T, device=dev), (z > 0).double()
+    for N in (12, 60):  # few rows, and tiles
+        zz = z.repeat(N // 12, 1)
+        y = api.linear_forward(zz, one, act=act)
+        assert torch.equal(y.double(), zz.double() * up.repeat(N // 12, 1)), act
+        dx, _, db = api.linear_backward(torch.ones_like(zz), zz, one, act=act, pre=zz, need_dw=False)
+        assert torch.equal(dx.double(), up.repeat(N // 12, 1)) and float(db) == N / 2, act
+        g = torch.cat([zz, torch.ones_like(zz)], 1)
+        w2 = torch.ones(2, 1, dtype=T, device=dev)
+        dx, _, db = api.gated_backward(torch.full_like(zz, 2.0 ** -64), zz, w2, g, act=act, need_dw=False)
+        assert torch.isfinite(dx).all() and float(db[0]) == N / 2 * 2.0 ** -64, act
