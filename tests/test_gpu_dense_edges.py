@@ -257,3 +257,69 @@ def test_activations_of_the_largest_numbers(dev, tname, act):
         w2 = torch.ones(2, 1, dtype=T, device=dev)
         dx, _, db = api.gated_backward(torch.full_like(zz, 2.0 ** -64), zz, w2, g, act=act, need_dw=False)
         assert torch.isfinite(dx).all() and float(db[0]) == N / 2 * 2.0 ** -64, act
+
+
+def test_small_loss_weights_in_fp16_by_value(dev):
+    """A weight of 2^-30 in fp16, with x or w so large that the gradients are
+    numbers that fp16 holds: all zeros would not do."""
+    T, c, N, Cs, Ct = torch.float16, 2.0 ** -30, 4096, 64, 40
+    for big_x in (True, False):
+        up = 2.0 ** 13
+        x = normal(dev, T, 1, N, Cs, scale=up if big_x else 1 / up)
+        w = normal(dev, T, 2, Ct, Cs, scale=(1 / up if big_x else up) / 8)
+        labels = torch.randint(0, Ct, (N,), generator=torch.Generator().manual_seed(3)).to(dev)
+        _, lse = api.linear_xent_forward(x, w, labels)
+        dx, dw, _ = api.linear_xent_backward(torch.full((N,), c, device=dev), lse, x, w, labels)
+        xd, wd = x.double(), w.double()
+        z = torch.mm(xd, wd.t())
+        p = torch.softmax(z, 1)
+        d = p.clone()
+        d[torch.arange(N, device=dev), labels] -= 1.0
+        d *= c
+        ez = 8 * math.sqrt(Cs) * E32 * torch.mm(xd.abs(), wd.abs().t()).max(1).values[:, None] + \
+            64 * E32 * (1 + z.abs().max())
+        # d / c is rounded to fp16 (times 2^10: subnormal half steps of 2^-35), the result too (2^-25)
+        off = 2.0 ** -11 * d.abs() + c * (2 * ez * p + 8 * E32 + 2.0 ** -35)
+        for got, ref, A, E, n, used in ((dw, torch.mm(d.t(), xd), torch.mm(d.abs().t(), xd.abs()),
+                                         torch.mm(off.t(), xd.abs()), N, big_x),
+                                        (dx, torch.mm(d, wd), torch.mm(d.abs(), wd.abs()), torch.mm(off, wd.abs()), Ct,
+                                         not big_x)):
+            if used:
+                bound = 8 * math.sqrt(n) * E32 * A + 2.0 ** -11 * ref.abs() + E + 2.0 ** -25
+                assert float((ref.abs() - bound).max()) > 0  # zeros would fail
+                near(got, ref, bound, "dw" if big_x else "dx")
+
+
+# One round of large tiles; parts of k; odd widths, so that dz's two halves
+# end within 16 bytes
+GATED = [(4096, 136, 2048), (2048, 256, 2000), (1030, 1000, 1031), (300, 2000, 77), (513, 520, 4003)]
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("N,Cs,Ct", GATED)
+def test_gated_gradients_of_every_cut(dev, tname, act, N, Cs, Ct):
+    T = TYPES[tname]
+    u = torch.finfo(T).eps / 2
+    x, w = normal(dev, T, 1, N, Cs), normal(dev, T, 2, 2 * Ct, Cs, scale=1 / math.sqrt(Cs))
+    dy, pre = normal(dev, T, 3, N, Ct), normal(dev, T, 4, N, 2 * Ct)
+    g, up, d = pre[:, :Ct].double(), pre[:, Ct:].double(), dy.double()
+    phi = 0.5 * torch.special.erfc(-g / math.sqrt(2.0)) if act == "gelu" else torch.sigmoid(g)
+    value = g * phi
+    slope = phi + g * (torch.exp(-0.5 * g * g) / math.sqrt(2.0 * math.pi) if act == "gelu" else phi * (1 - phi))
+    dz = torch.cat([d * up * slope, d * value], 1)
+    size = torch.cat([d.abs() * up.abs(), d.abs() * g.abs()], 1)  # what an fp32 rounding is relative to
+    off = u * dz.abs() + 16 * E32 * size + (2.0 ** -25 if T == torch.float16 else 0)
+    print("gated gradients", tname, act, N, Cs, Ct, flush=True)
+    dx, dw, db = api.gated_backward(dy, x, w, pre, act=act)
+    xd, wd = x.double(), w.double()
+    tiny = 2.0 ** -25 if T == torch.float16 else 0
+
+    def bound(n, A, ref):
+        return 8 * math.sqrt(n) * E32 * A + u * ref.abs() + 16 * E32 * ref.abs() + tiny
+
+    ref = torch.mm(dz, wd)
+    near(dx, ref, bound(2 * Ct, torch.mm(dz.abs(), wd.abs()), ref) + torch.mm(off, wd.abs()), "dx")
+    ref = torch.mm(dz.t(), xd)
+    near(dw, ref, bound(N, torch.mm(dz.abs().t(), xd.abs()), ref) + torch.mm(off.t(), xd.abs()), "dw")
+    near(db, dz.sum(0), bound(N, dz.abs().sum(0), dz.sum(0)) + 16 * E32 * size.sum(0), "dbias")
