@@ -361,7 +361,10 @@ qcnn_status qcnn_ec_conv(const float* S, int N, int C_s, int H, int W,
  * Types: `dtype` is the type T of every array declared void* (fp32, bf16 or
  * fp16); sums, softmax statistics, loss and lse are fp32; a result is rounded
  * to T once.  The backward calls round one intermediate to T as well, the
- * operand of the matrix products (dz; the logits' gradient).
+ * operand of the matrix products (dz; the logits' gradient, of which dbias of
+ * the loss is the sum too): 16-bit gradients have two roundings, 1.4 times the
+ * error of one.  In fp32, products of more than 32 rows see their operands to
+ * 24 bits or to a multiple of 2^-133, whichever is coarser.
  * Layouts: x [N][C_s], w [C_t][C_s], y, dy, residual [N][C_t].  x, y, dy and
  * residual have row strides ldx, ldy, lddy, ldr in elements (at least their
  * columns); everything else is contiguous.  Pointers are aligned to their

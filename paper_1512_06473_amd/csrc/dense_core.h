@@ -311,6 +311,8 @@ __device__ __forceinline__ f4 class_logits(int np, int p, f4 v, f4 bias) {
 // that read d multiply it back) so that a mean's 1 / N neither leaves a 16-bit
 // type's range nor rounds every label's entry the same way; times `gain`, a
 // power of two that keeps fp16's small probabilities off its subnormals.
+// Rounded to T, which is what the products take; its column sums are made from
+// the rounded entries, too (the tiles of a column do not meet).
 // y's rows are whole quads: what lies past np is written as 0.
 template <typename T, int U>
 __device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int nq, int q, int dq, int p, f4 (&z)[U], f4 bias) {
@@ -347,7 +349,9 @@ __device__ __forceinline__ void emit_xgrad(const Epi& e, int np, int nq, int q, 
 
 // (max, sum of exp(. - max)) of two disjoint sets.  fmaxf passes over NaN: the
 // sum is what carries it.  A set whose maximum is -inf is empty or masked and
-// has the sum 0, or NaN where a logit was that; either is added as it is.
+// has the sum 0, or NaN where a logit was that; either is added as it is.  The
+// hardware's exponential in fp32 too: it is off by |x| 2^-24 of exp(x), that is
+// a sum of C exponentials by log(C) 2^-24 of itself at most, and lse by as much.
 __device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
   const float sa = a.x == -INFINITY ? a.y : a.y * __expf(a.x - m);
@@ -702,13 +706,15 @@ __device__ __forceinline__ void finish_tile(const Prod& a, const Epi& e, const P
 // (256 x 256, 8 waves of 128 x 64): a step is 64 MFMA per wave for 24 LDS reads
 // of 16 bytes and 8 loads; a larger tile than 128 x 128 halves the LDS and L2
 // bytes per product, and 64 KB a step twice is what LDS holds.  Bound by the
-// matrix cores and the chip's power: 8192 x 4096 -> 16384 in bf16 takes 825 us
-// (1330 TFLOP/s), its input gradient 790, its weight gradient 815, at 1.6 to 2
-// GHz.  Without the half-step prefetch 1128 us, results stored in the products'
-// order (not through LDS) 1060, 128 x 128 tiles 1185; with a step's scalar work
-// and loads in a block behind the barrier 865, not between the products.  Four
-// waves of 128 x 128 spill their sums between the two register files (1140 us);
-// 32 x 32 MFMA are 5 % slower.
+// matrix cores and the chip's power: 8192 x 4096 -> 16384 in bf16 takes 901 us
+// in 50 calls in a row (1220 TFLOP/s), its input gradient 866, its weight
+// gradient 873; single calls 860 to 1130 as the clock, 1.4 to 1.9 GHz, has it.
+// The way there, in short runs of one day, which end at 825 us: 128 x 128 tiles
+// 1185; 256 x 256 1128; with the half-step prefetch 1060; with results through
+// LDS, not stored in the products' order, 955, and other steps 865; with a
+// step's scalar work and loads between the products, not in a block behind the
+// barrier, 825.  Four waves of 128 x 128 spill their sums between the two
+// register files (1140 us); 32 x 32 MFMA are 5 % slower.
 // Bounded to 512 threads also where 256 run: with more than 256 registers to
 // give, the compiler keeps the sums in the other file and moves them around in
 // every turn of the loop (512 x 4096 -> 4096: 29.2 us, so 28.2).
@@ -924,11 +930,12 @@ struct Planes {
 };
 
 // Large tiles 256 x 128 (8 waves of 64 x 64), small ones 128 x 128 (of 64 x 32).
-// Bound by the matrix cores and power: 4096 x 4096 -> 4096 takes 670 us forward,
-// 608 and 585 for the gradients (205 to 235 TFLOP/s, that is 1230 to 1410 of
-// bf16 products).  Fp32's own instruction 970, split where the fragments are
-// read 712 to 765, split in blocks before and after the products of a row 720,
-// 625 and 617.
+// Bound by the matrix cores and power: 4096 x 4096 -> 4096 takes 639 us forward
+// in 50 calls in a row, 647 and 645 for the gradients (215 TFLOP/s, that is 1290
+// of bf16 products); single calls 630 to 720.  The way there, in short runs:
+// fp32's own instruction 970, split where the fragments are read 712 to 765,
+// split in blocks before and after the products of a row 720 (gradients 625 and
+// 617), between them one by one 670 (608 and 585).
 template <bool PS, bool QS, int BP, int BQ, int WP, int WQ, int EPI, bool GATED>
 __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ)) void product_f32_kernel(const Prod a, const Epi e) {
 #ifdef __HIP_DEVICE_COMPILE__

@@ -62,6 +62,8 @@ __global__ __launch_bounds__(256) void pad_kernel(const T* __restrict__ src, lon
 // thread has 16 bytes of columns and goes down `chunk` rows, the loads of 4 at
 // a time; the sums of a block's rows go to part[blockIdx.y][columns of dz],
 // joined by colsum_kernel: the order of the additions is the same in every run.
+// dz is rounded to T for the products, whose instructions take 16-bit operands
+// (two parts of it would double their time); the sums are of dz unrounded.
 struct Slope {
   const void* dy;
   const void* pre;
