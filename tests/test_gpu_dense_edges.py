@@ -1,6 +1,7 @@
 """The dense layers where numbers run out: NaN among a row's logits, loss
 weights and activations at the ends of their range, fp32's accuracy in one
-sign, and gradients of a size that a 16-bit type still holds.
+sign, gradients of a size that a 16-bit type still holds, and the largest
+sizes.
 
 References are float64; tolerances count half steps of 2^-24 (fp32) or of the
 type, as in test_gpu_dense.py, and are derived at each test.
@@ -323,3 +324,83 @@ def test_gated_gradients_of_every_cut(dev, tname, act, N, Cs, Ct):
     ref = torch.mm(dz.t(), xd)
     near(dw, ref, bound(N, torch.mm(dz.abs().t(), xd.abs()), ref) + torch.mm(off.t(), xd.abs()), "dw")
     near(db, dz.sum(0), bound(N, dz.abs().sum(0), dz.sum(0)) + 16 * E32 * size.sum(0), "dbias")
+
+
+@pytest.mark.parametrize("tname", list(TYPES))
+@pytest.mark.parametrize("N,Cs,Ct", [(1 << 21, 8, 18), (1 << 21, 7, 5), (4, 1 << 20, 6), (40, 1 << 20, 6),
+                                     (4, 6, 1 << 20), (40, 6, 1 << 20)])
+def test_the_largest_sizes(dev, tname, N, Cs, Ct):
+    """2^21 rows, 2^20 columns: every call at the limits that the header names."""
+    T = TYPES[tname]
+    u = torch.finfo(T).eps / 2
+    tiny = 2.0 ** -25 if T == torch.float16 else 0  # half of fp16's smallest number
+    big = max(N, Cs, Ct) ** -0.25                   # keeps fp16's sums of 2^21 terms in range
+    x, w, dy = (normal(dev, T, k, *s, scale=big) for k, s in enumerate([(N, Cs), (Ct, Cs), (N, Ct)]))
+    xd, wd, dyd = x.double(), w.double(), dy.double()
+    print("largest", tname, N, Cs, Ct, flush=True)
+
+    def bound(n, a, b, ref):
+        return 8 * math.sqrt(n) * E32 * torch.mm(a.abs(), b.abs()) + (u + 4 * E32) * ref.abs() + tiny
+
+    ref = torch.mm(xd, wd.t())
+    near(api.linear_forward(x, w), ref, bound(Cs, xd, wd.t(), ref), "y")
+    half = Ct // 2
+    if half * 2 == Ct:
+        e = bound(Cs, xd, wd.t(), ref) - (u + 4 * E32) * ref.abs() - tiny
+        g, up = ref[:, :half], ref[:, half:]
+        want = g.clamp(min=0) * up
+        near(api.gated_forward(x, w, act="relu"), want,
+             e[:, :half] * (up.abs() + e[:, half:]) + e[:, half:] * g.abs() + (u + 8 * E32) * want.abs() + tiny, "gated")
+    dx, dw, db = api.linear_backward(dy, x, w)
+    ref = torch.mm(dyd, wd)
+    near(dx, ref, bound(Ct, dyd, wd, ref), "dx")
+    ref = torch.mm(dyd.t(), xd)
+    near(dw, ref, bound(N, dyd.t(), xd, ref), "dw")
+    ref = dyd.sum(0)
+    near(db, ref, 8 * math.sqrt(N) * E32 * dyd.abs().sum(0) + (u + 4 * E32) * ref.abs() + tiny, "dbias")
+    del ref
+    labels = torch.arange(N, device=dev) % Ct
+    z = torch.mm(xd, wd.t())
+    lse = torch.logsumexp(z, 1)
+    loss, glse = api.linear_xent_forward(x, w, labels)
+    ez = 8 * math.sqrt(Cs) * E32 * torch.mm(xd.abs(), wd.abs().t()).max(1).values + 32 * E32 * (1 + z.abs().max() + lse.abs())
+    near(glse, lse, ez, "lse")
+    near(loss, lse - z.gather(1, labels[:, None])[:, 0], 2 * ez + E32 * lse.abs(), "loss")
+    gx, gw, gb = api.linear_xent_backward(torch.full((N,), 1.0, device=dev), glse, x, w, labels, need_dbias=True)
+    p = torch.softmax(z, 1)
+    d = p.clone()
+    d.scatter_add_(1, labels[:, None], torch.full((N, 1), -1.0, device=dev, dtype=torch.float64))
+    # d is rounded to T (fp16: times 2^10, subnormal half steps 2^-35); logits and lse are off by ez each
+    off = u * d.abs() + p * (2 * ez)[:, None] + 8 * E32 * d.abs() + (2.0 ** -35 if T == torch.float16 else 0)
+    ref = torch.mm(d, wd)
+    near(gx, ref, bound(Ct, d, wd, ref) + torch.mm(off, wd.abs()), "loss dx")
+    ref = torch.mm(d.t(), xd)
+    near(gw, ref, bound(N, d.t(), xd, ref) + torch.mm(off.t(), xd.abs()), "loss dw")
+    ref = d.sum(0)
+    near(gb, ref, 8 * math.sqrt(N) * E32 * d.abs().sum(0) + (u + 4 * E32) * ref.abs() + off.sum(0) + tiny, "loss dbias")
+
+
+def test_two_threads_on_one_stream(dev):
+    """Calls that share the stream's workspace (copies, split sums, sums of
+    columns), enqueued by two threads at once: each as if it were alone."""
+    import threading
+    jobs = []
+    for k, (N, Cs, Ct) in enumerate([(200, 1001, 130), (129, 65, 77)]):
+        x, w, dy = (normal(dev, torch.bfloat16, 3 * k + i, *s) for i, s in enumerate([(N, Cs), (Ct, Cs), (N, Ct)]))
+        jobs.append((x, w, dy, [api.linear_forward(x, w), *api.linear_backward(dy, x, w)]))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(x, w, dy, want):
+        for _ in range(40):
+            got = [api.linear_forward(x, w), *api.linear_backward(dy, x, w)]
+            torch.cuda.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                wrong.append(tuple(x.shape))
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
